@@ -335,6 +335,105 @@ int locmoe_expert_ffn_wgrad(const locmoe_desc* desc, const void* send, const voi
 int locmoe_dispatch_bwd(const locmoe_desc* desc, const void* dsend, const int32_t* slot, const float* dg,
                         void* dx, void* stream);
 
+/* ---- The layer in a transformer block ---------------------------------------------------------------------
+ * What stands between the layer and the residual stream x of a block,
+ *   y = x + scale w gamma_out n(out),   out the expert's output for the normalised token n(x) gamma_in,
+ *   n(v) = v r,  r = 1 / sqrt(mean_j v_j^2 + norm_eps)   (root-mean-square norm over the d features of a row),
+ * forward and backward, each in one pass with the step of the path beside it.  The norm behind the layer stands ahead of
+ * the score w: a norm of w out would cancel w, and the router's gradient with it.
+ * Sums and products in fp32; xn, y, dout and dx are rounded once, to x_dtype.  gamma_in, gamma_out: device [d] fp32, NULL
+ * means ones.  Finite rows whose squares overflow fp32 (values above some 1e18) give r = 0.
+ * A row is at most LOCMOE_NORM_MAX_ROW_BYTES long (d <= 32 768 in bf16, 16 384 in fp32), else LOCMOE_ERR_SHAPE. */
+#define LOCMOE_NORM_MAX_ROW_BYTES 65536
+
+/* Bytes of device scratch for the gradients of gamma_in and gamma_out (one buffer serves both backward steps: they do not
+ * overlap in time on one stream; nothing in it has to be set).  0 on an invalid descriptor or a longer row. */
+size_t locmoe_norm_workspace_bytes(const locmoe_desc* desc);
+
+/* The norm ahead of the layer, and the gating value (Eq. 4) of its result:
+ *   xn[m,j] = x[m,j] r_m gamma[j];   rstd[m] = r_m;   g[m,i] = mean of the i-th block of d/E features of xn[m,:].
+ *   g is the mean of the values before their rounding to x_dtype (locmoe_gate of xn: of the rounded ones).
+ *   x device [T,d] of x_dtype (read); xn device [T,d] of x_dtype (written, may be x itself); rstd device [T] fp32 or NULL;
+ *   g device [T,E] fp32 or NULL (another gate follows).  LOCMOE_ERR_ARG unless norm_eps is finite and > 0. */
+int locmoe_norm_gate(const locmoe_desc* desc, const void* x, const float* gamma, float norm_eps, void* xn, float* rstd,
+                     float* g, void* stream);
+
+/* Combine (Eq. 1 with the score of Eq. 3), the norm behind the layer, the residual:
+ *   y[m,j] = res[m,j] + scale w[m] gamma[j] r_m out[slot[m],j],  r_m of the row out[slot[m],:] (post_norm = 1) or 1 (0);
+ *   y[m,:] = res[m,:], bit for bit, for a dropped token (slot[m] < 0).   rstd[m] = r_m, 0 for a dropped token.
+ *   out device [E*C,d] of x_dtype; slot device [T] i32; w device [T] fp32; res device [T,d] of x_dtype; y device [T,d] of
+ *   x_dtype (every row written, may be res itself); rstd device [T] fp32 or NULL.  LOCMOE_ERR_ARG unless scale is finite and,
+ *   with post_norm, norm_eps finite and > 0. */
+int locmoe_combine_norm(const locmoe_desc* desc, const void* out, const int32_t* slot, const float* w, const void* res,
+                        const float* gamma, int32_t post_norm, float norm_eps, float scale, void* y, float* rstd,
+                        void* stream);
+
+/* locmoe_combine_norm, backward.  With n = r_m out[slot[m],:] and u = scale gamma dy[m,:], for a kept token:
+ *   dw[m] = <u, n>;   dout[slot[m],:] = r_m w[m] (u - n dw[m] / d)  (post_norm; else w[m] u);
+ *   dgamma[j] = sum_m scale w[m] dy[m,j] n[j].  dw[m] = 0 for a dropped token, whose dy row is not read.  (The residual's
+ *   gradient is dy itself: locmoe_dispatch_norm_bwd takes it.)
+ *   rstd device [T] fp32 from locmoe_combine_norm (not read, may be NULL, if post_norm = 0); dout device [E*C,d] of x_dtype
+ *   (rows [0,K) written); dw device [T] fp32; dgamma device [d] fp32 or NULL (then ws is not looked at); ws device scratch
+ *   of >= locmoe_norm_workspace_bytes.  Sums run in a fixed order: the same bits every time. */
+int locmoe_combine_norm_bwd(const locmoe_desc* desc, const void* dy, const void* out, const int32_t* slot, const float* w,
+                            const float* gamma, int32_t post_norm, float scale, const float* rstd, void* dout, float* dw,
+                            float* dgamma, void* ws, size_t ws_bytes, void* stream);
+
+/* The dispatch permutation, Eq. 4 and the norm ahead of the layer, backward, and the residual's gradient.  With
+ * dxn[m,j] = (slot[m] >= 0 ? dsend[slot[m],j] : 0) + (E/d) dg[m, j / (d/E)] and xh = x r_m:
+ *   dx[m,j] = dres[m,j] + r_m (gamma[j] dxn[m,j] - xh[j] mean_k(gamma[k] dxn[m,k] xh[k]));   dgamma[j] = sum_m dxn[m,j] xh[j].
+ *   dsend device [E*C,d] and x, dx device [T,d] of x_dtype (every dx row written; dx may be dres or x itself); dg device
+ *   [T,E] fp32 from locmoe_route_bwd; rstd device [T] fp32 from locmoe_norm_gate; dres device [T,d] of x_dtype or NULL (no
+ *   residual); dgamma, ws as above. */
+int locmoe_dispatch_norm_bwd(const locmoe_desc* desc, const void* dsend, const int32_t* slot, const float* dg,
+                             const void* x, const float* gamma, const float* rstd, const void* dres, void* dx,
+                             float* dgamma, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- The layer for a few tokens ----------------------------------------------------------------------------
+ * Gate, top-1, score, first-come capacity, expert FFN and combine for T <= LOCMOE_FEW_MAX_TOKENS tokens in two launches, as
+ * decoding calls the layer (no statistics and no send buffer):
+ *   eid, w as locmoe_route;   slot[m] = m if fewer than C tokens before m have the same expert, else -1 (dropped);
+ *   y[m,:] = w[m] out_m (zeros for a dropped token) with weighted = 1;  with weighted = 0 out_m itself, rows of dropped
+ *   tokens left as they are: y and slot then are what locmoe_combine and locmoe_combine_norm take.
+ *   out_m = W_out[e] . GeLU(W_in[e] . x_m).  bf16 storage: H rounded to bf16, y once; fp32 storage: the activations enter with
+ *   all 24 bits (down to 2^-109 in magnitude) and H stays in fp32 precision, unlike locmoe_expert_ffn, which rounds both to
+ *   bf16.  The order of the sums depends on T and the routing, so bits may differ from the other path's, and a token's with
+ *   the batch it is in; the same call gives the same bits.
+ *   x device [T,d] of x_dtype; g device [T,E] fp32 (gating values from locmoe_norm_gate or locmoe_gate_dense) or NULL (formed
+ *   here as locmoe_gate does, up to the order of the additions); eps device [E] fp32 or NULL; W_in, W_out row-major or packed
+ *   as desc->w_packed says; eid, slot device [T] i32, w device [T] fp32, y device [T,d] of x_dtype (may be x itself);
+ *   ws device scratch of >= locmoe_layer_few_workspace_bytes (0: an invalid descriptor, or too many tokens), nothing in it
+ *   has to be set.  desc->N, alpha and mu are not used.  LOCMOE_ERR_SHAPE if T > LOCMOE_FEW_MAX_TOKENS. */
+#define LOCMOE_FEW_MAX_TOKENS 64
+size_t locmoe_layer_few_workspace_bytes(const locmoe_desc* desc);
+int locmoe_layer_few(const locmoe_desc* desc, const void* x, const float* g, const float* eps, const void* W_in,
+                     const void* W_out, int32_t weighted, int32_t* eid, float* w, int32_t* slot, void* y, void* ws,
+                     size_t ws_bytes, void* stream);
+
+/* ---- Hidden activations kept in 8 bits -----------------------------------------------------------------------
+ * The training forward and the data gradients with the pre-activation kept in 9 bits a value in place of Z and H (32 bits):
+ * per row and block of 16 columns (the last one shorter if h % 16 != 0)
+ *   Zs = max |z| / 127, rounded to bf16;   Zq = z / Zs, rounded to the nearest whole number, |Zq| <= 127;
+ * what is kept stands for Zq Zs: at most Zs / 2 from z.  A block with an infinity or a NaN reads back as NaN, one whose
+ * largest value is below 1.5e-36 as zeros.  H_ws is scratch on both sides: between the two calls only Zq and Zs are kept.
+ *   Zq device [E*C,h] int8, Zs device [E*C, ceil(h/16)] bf16 (rows [0,K) written).
+ *   _in_save8:  H_ws = GeLU(z) of the unrounded z, as locmoe_expert_ffn_in, for locmoe_expert_ffn_out.
+ *   _dgrad8:    as locmoe_expert_ffn_dgrad with Z = Zq Zs, and H_ws[r,:] = GeLU(Zq Zs) (bf16, rows [0,K) written), which
+ *               locmoe_expert_ffn_wgrad takes for H.
+ * Everything else, the *_ws forms included, as without the 8. */
+int locmoe_expert_ffn_in_save8(const locmoe_desc* desc, const void* send, const int32_t* seg_off, const int32_t* buf_expert,
+                               const void* W_in, void* H_ws, int8_t* Zq, void* Zs, void* stream);
+int locmoe_expert_ffn_dgrad8(const locmoe_desc* desc, const void* dout, const int8_t* Zq, const void* Zs,
+                             const int32_t* seg_off, const int32_t* buf_expert, const void* W_out_t, const void* W_in_t,
+                             void* dZ, void* H_ws, void* dsend, void* stream);
+int locmoe_expert_ffn_in_save8_ws(const locmoe_desc* desc, const void* send, const int32_t* seg_off,
+                                  const int32_t* buf_expert, const void* W_in, void* H_ws, int8_t* Zq, void* Zs, void* ws,
+                                  size_t ws_bytes, void* stream);
+int locmoe_expert_ffn_dgrad8_ws(const locmoe_desc* desc, const void* dout, const int8_t* Zq, const void* Zs,
+                                const int32_t* seg_off, const int32_t* buf_expert, const void* W_out_t,
+                                const void* W_in_t, void* dZ, void* H_ws, void* dsend, void* ws, size_t ws_bytes,
+                                void* stream);
+
 #ifdef __cplusplus
 }
 #endif

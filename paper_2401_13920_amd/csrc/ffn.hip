@@ -200,7 +200,7 @@ __device__ __forceinline__ void dma_prefill(const DmaTile& t, const DmaLane& ln,
 // direct-to-LDS loads do not retire in order relative to each other, so no smaller count is safe there).
 template <int NJ, int EPI, class F>
 __device__ __forceinline__ void dma_tile(const DmaTile& cur, const DmaTile& nxt, const DmaLane& ln, DmaRing& ring,
-                                         uint16_t* __restrict__ Cout, uint16_t* aux, uint32_t lds0, int KD, int wm, int wn,
+                                         uint16_t* __restrict__ Cout, AuxOf<EPI> aux, uint32_t lds0, int KD, int wm, int wn,
                                          int lane, int wave, int ldc, F&& before_epilogue) {
   // NJ = live 16-row activation subtiles of this wave
   constexpr int NLO = NJ < 4 ? NJ : 4;        // first group of subtiles
@@ -340,7 +340,7 @@ __device__ __forceinline__ void dma_tile(const DmaTile& cur, const DmaTile& nxt,
 // one-subtile variant on clamped rows and stores nothing
 template <int EPI, class F>
 __device__ __forceinline__ void dma_tile_any(const DmaTile& cur, const DmaTile& nxt, const DmaLane& ln, DmaRing& ring,
-                                             uint16_t* __restrict__ Cout, uint16_t* aux, uint32_t lds0, int KD, int lane, int wave,
+                                             uint16_t* __restrict__ Cout, AuxOf<EPI> aux, uint32_t lds0, int KD, int lane, int wave,
                                              int ldc, F&& before_epilogue) {
   const int wm = wave >> 1, wn = wave & 1;
   const int nsub = min(16, (cur.rows_left + 15) >> 4);  // live 16-row subtiles of this tile
@@ -364,7 +364,7 @@ __device__ __forceinline__ void dma_tile_any(const DmaTile& cur, const DmaTile& 
 template <int EPI>
 __global__ __launch_bounds__(kDmaThreads) void ffn_gemm_dma(const uint16_t* __restrict__ A,
                                                             const uint16_t* __restrict__ Wp,
-                                                            uint16_t* __restrict__ Cout, uint16_t* aux,
+                                                            uint16_t* __restrict__ Cout, AuxOf<EPI> aux,
                                                             const int32_t* __restrict__ seg_off,
                                                             const int32_t* __restrict__ buf_expert, int Kdim,
                                                             int Ndim, int MT, int NT) {
@@ -423,7 +423,7 @@ __device__ __forceinline__ void leave_queues(unsigned int* queue, unsigned group
 template <int EPI>
 __global__ __launch_bounds__(kDmaThreads) void ffn_gemm_dma_persistent(const uint16_t* __restrict__ A,
                                                                        const uint16_t* __restrict__ Wp,
-                                                                       uint16_t* __restrict__ Cout, uint16_t* aux,
+                                                                       uint16_t* __restrict__ Cout, AuxOf<EPI> aux,
                                                                        const int32_t* __restrict__ seg_off,
                                                                        const int32_t* __restrict__ buf_expert,
                                                                        int Kdim, int Ndim, int NT, int E,
@@ -540,7 +540,7 @@ constexpr int kFewRows = 32, kFewCols = 64, kFewDepth = 8;  // (k-steps in fligh
 
 template <int NJ, int EPI>
 __global__ __launch_bounds__(64, 1) void ffn_gemm_few(const uint16_t* __restrict__ A, const uint16_t* __restrict__ Wp,
-                                                      uint16_t* __restrict__ Cout, uint16_t* aux,
+                                                      uint16_t* __restrict__ Cout, AuxOf<EPI> aux,
                                                       const int32_t* __restrict__ seg_off,
                                                       const int32_t* __restrict__ buf_expert, int Kdim, int Ndim) {
   constexpr int D = kFewDepth;
@@ -730,7 +730,7 @@ PackedKernel pick_packed(int E, int rows_max, int T, int Kdim, int Ndim, bool ke
 }
 
 template <int EPI>
-int launch_dma(const void* A, const void* Wp, void* C, void* aux, const int32_t* seg_off, const int32_t* buf_expert, int E,
+int launch_dma(const void* A, const void* Wp, void* C, AuxOf<EPI> aux, const int32_t* seg_off, const int32_t* buf_expert, int E,
                int rows_max, int T, int Kdim, int Ndim, unsigned int* queue, hipStream_t st) {
   const int MT = ceil_div(rows_max, kBM), NT = Ndim / kBN;
   const long long total = (long long)E * MT * NT;
@@ -739,7 +739,7 @@ int launch_dma(const void* A, const void* Wp, void* C, void* aux, const int32_t*
   if (pick == PackedKernel::kFew) {
     auto few = rows_max <= 16 ? ffn_gemm_few<1, EPI> : ffn_gemm_few<2, EPI>;
     hipLaunchKernelGGL(few, dim3((unsigned)(E * (Ndim / kFewCols))), dim3(64), 0, st, (const uint16_t*)A,
-                       (const uint16_t*)Wp, (uint16_t*)C, (uint16_t*)aux, seg_off, buf_expert, Kdim, Ndim);
+                       (const uint16_t*)Wp, (uint16_t*)C, aux, seg_off, buf_expert, Kdim, Ndim);
     return launch_status();
   }
   if (pick == PackedKernel::kAny)
@@ -752,13 +752,13 @@ int launch_dma(const void* A, const void* Wp, void* C, void* aux, const int32_t*
     // (up to four work-groups per tile of the upper bound: the kernel cuts the m-tiles of a short list finer)
     const long long groups = std::min<long long>((cu_count() / 8) * 8, (4 * total + 7) / 8 * 8);
     hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(kDmaThreads), kDmaSmem, st, (const uint16_t*)A,
-                       (const uint16_t*)Wp, (uint16_t*)C, (uint16_t*)aux, seg_off, buf_expert, Kdim, Ndim, NT, E, queue);
+                       (const uint16_t*)Wp, (uint16_t*)C, aux, seg_off, buf_expert, Kdim, Ndim, NT, E, queue);
     return launch_status();
   }
   auto kern = ffn_gemm_dma<EPI>;
   if (!allow_lds((const void*)kern, kDmaSmem, lds_allowed[1])) return LOCMOE_ERR_HIP;
   hipLaunchKernelGGL(kern, dim3((unsigned)total), dim3(kDmaThreads), kDmaSmem, st, (const uint16_t*)A,
-                     (const uint16_t*)Wp, (uint16_t*)C, (uint16_t*)aux, seg_off, buf_expert, Kdim, Ndim, MT, NT);
+                     (const uint16_t*)Wp, (uint16_t*)C, aux, seg_off, buf_expert, Kdim, Ndim, MT, NT);
   return launch_status();
 }
 
@@ -809,7 +809,7 @@ namespace {
 // the packed-weight kernel, or nullptr (fixed tile assignment).
 template <int EPI>
 int gemm_d_to_h(const locmoe_desc* desc, const void* A, const int32_t* seg_off, const int32_t* buf_expert,
-                const void* W, void* Cbf16, void* aux, unsigned int* queue, void* stream) {
+                const void* W, void* Cbf16, AuxOf<EPI> aux, unsigned int* queue, void* stream) {
   const int rows_max = desc->C < desc->T ? desc->C : desc->T;  // kept[e] <= min(C, T)
   if (desc->w_packed) {
     if (desc->x_dtype != LOCMOE_BF16 || !packable(desc)) return LOCMOE_ERR_ARG;
@@ -853,7 +853,7 @@ int ffn_in(const locmoe_desc* desc, const void* send, const int32_t* seg_off, co
   if (!desc || !send || !seg_off || !buf_expert || !W_in || !H_ws) return LOCMOE_ERR_NULL;
   const int st = check_desc(desc);
   if (st != LOCMOE_OK) return st;
-  if (Z) return gemm_d_to_h<kEpiGeluSave>(desc, send, seg_off, buf_expert, W_in, H_ws, Z, queue_set(ws, 0), stream);
+  if (Z) return gemm_d_to_h<kEpiGeluSave>(desc, send, seg_off, buf_expert, W_in, H_ws, (uint16_t*)Z, queue_set(ws, 0), stream);
   return gemm_d_to_h<kEpiGelu>(desc, send, seg_off, buf_expert, W_in, H_ws, nullptr, queue_set(ws, 0), stream);
 }
 
@@ -872,10 +872,33 @@ int ffn_dgrad(const locmoe_desc* desc, const void* dout, const void* Z, const in
   int st = check_desc(desc);
   if (st != LOCMOE_OK) return st;
   // dZ = (dout . W_out) * GeLU'(Z): W_out^T is [h,d], the orientation of W_in
-  st = gemm_d_to_h<kEpiGeluGrad>(desc, dout, seg_off, buf_expert, W_out_t, dZ, const_cast<void*>(Z), queue_set(ws, 0),
+  st = gemm_d_to_h<kEpiGeluGrad>(desc, dout, seg_off, buf_expert, W_out_t, dZ, (uint16_t*)const_cast<void*>(Z), queue_set(ws, 0),
                                  stream);
   if (st != LOCMOE_OK) return st;
   // dsend = dZ . W_in: W_in^T is [d,h], the orientation of W_out
+  return gemm_h_to_d(desc, dZ, seg_off, buf_expert, W_in_t, dsend, queue_set(ws, 1), stream);
+}
+
+int ffn_in8(const locmoe_desc* desc, const void* send, const int32_t* seg_off, const int32_t* buf_expert, const void* W_in,
+            void* H_ws, int8_t* Zq, void* Zs, void* ws, void* stream) {
+  if (!desc || !send || !seg_off || !buf_expert || !W_in || !H_ws || !Zq || !Zs) return LOCMOE_ERR_NULL;
+  const int st = check_desc(desc);
+  if (st != LOCMOE_OK) return st;
+  return gemm_d_to_h<kEpiGeluSave8>(desc, send, seg_off, buf_expert, W_in, H_ws, Act8{Zq, (uint16_t*)Zs, nullptr},
+                                    queue_set(ws, 0), stream);
+}
+
+int ffn_dgrad8(const locmoe_desc* desc, const void* dout, const int8_t* Zq, const void* Zs, const int32_t* seg_off,
+               const int32_t* buf_expert, const void* W_out_t, const void* W_in_t, void* dZ, void* H_ws, void* dsend,
+               void* ws, void* stream) {
+  if (!desc || !dout || !Zq || !Zs || !seg_off || !buf_expert || !W_out_t || !W_in_t || !dZ || !H_ws || !dsend)
+    return LOCMOE_ERR_NULL;
+  int st = check_desc(desc);
+  if (st != LOCMOE_OK) return st;
+  st = gemm_d_to_h<kEpiGeluGrad8>(desc, dout, seg_off, buf_expert, W_out_t, dZ,
+                                  Act8{const_cast<int8_t*>(Zq), (uint16_t*)const_cast<void*>(Zs), (uint16_t*)H_ws},
+                                  queue_set(ws, 0), stream);
+  if (st != LOCMOE_OK) return st;
   return gemm_h_to_d(desc, dZ, seg_off, buf_expert, W_in_t, dsend, queue_set(ws, 1), stream);
 }
 
@@ -976,6 +999,34 @@ extern "C" int locmoe_expert_ffn_ws(const locmoe_desc* desc, const void* send, c
   const int st = ffn_in(desc, send, seg_off, buf_expert, W_in, H_ws, nullptr, ws, stream);
   if (st != LOCMOE_OK) return st;
   return ffn_out(desc, H_ws, seg_off, buf_expert, W_out, out, ws, stream);
+}
+
+// ---- pre-activations kept in 8 bits ------------------------------------------------------------------------------
+extern "C" int locmoe_expert_ffn_in_save8(const locmoe_desc* desc, const void* send, const int32_t* seg_off,
+                                          const int32_t* buf_expert, const void* W_in, void* H_ws, int8_t* Zq, void* Zs,
+                                          void* stream) {
+  return ffn_in8(desc, send, seg_off, buf_expert, W_in, H_ws, Zq, Zs, nullptr, stream);
+}
+
+extern "C" int locmoe_expert_ffn_in_save8_ws(const locmoe_desc* desc, const void* send, const int32_t* seg_off,
+                                             const int32_t* buf_expert, const void* W_in, void* H_ws, int8_t* Zq, void* Zs,
+                                             void* ws, size_t ws_bytes, void* stream) {
+  if (!ws_ok(ws, ws_bytes)) return LOCMOE_ERR_WORKSPACE;
+  return ffn_in8(desc, send, seg_off, buf_expert, W_in, H_ws, Zq, Zs, ws, stream);
+}
+
+extern "C" int locmoe_expert_ffn_dgrad8(const locmoe_desc* desc, const void* dout, const int8_t* Zq, const void* Zs,
+                                        const int32_t* seg_off, const int32_t* buf_expert, const void* W_out_t,
+                                        const void* W_in_t, void* dZ, void* H_ws, void* dsend, void* stream) {
+  return ffn_dgrad8(desc, dout, Zq, Zs, seg_off, buf_expert, W_out_t, W_in_t, dZ, H_ws, dsend, nullptr, stream);
+}
+
+extern "C" int locmoe_expert_ffn_dgrad8_ws(const locmoe_desc* desc, const void* dout, const int8_t* Zq, const void* Zs,
+                                           const int32_t* seg_off, const int32_t* buf_expert, const void* W_out_t,
+                                           const void* W_in_t, void* dZ, void* H_ws, void* dsend, void* ws,
+                                           size_t ws_bytes, void* stream) {
+  if (!ws_ok(ws, ws_bytes)) return LOCMOE_ERR_WORKSPACE;
+  return ffn_dgrad8(desc, dout, Zq, Zs, seg_off, buf_expert, W_out_t, W_in_t, dZ, H_ws, dsend, ws, stream);
 }
 
 extern "C" int locmoe_transpose_weights(const locmoe_desc* desc, const void* W_in, const void* W_out, void* W_in_t,

@@ -4,13 +4,14 @@
 #include <math.h>
 #include <stdint.h>
 
+#include "ffn_epilogue.h"
 #include "locmoe.h"
 
 namespace locmoe {
 
 // C[rows, N] = epilogue(A[rows, K] . W[N, K]^T) per segment; rows_max: rows per segment at most, T: tokens (rows in all)
 template <bool A_F32, bool PACKED, int EPI, bool OUT_F32>
-int any_gemm(const void* A, const void* W, void* C, void* aux, const int32_t* seg_off, const int32_t* buf_expert, int E,
+int any_gemm(const void* A, const void* W, void* C, AuxOf<EPI> aux, const int32_t* seg_off, const int32_t* buf_expert, int E,
              int rows_max, int T, int Kdim, int Ndim, hipStream_t st);
 
 // the largest of three times that overlap, a little more where they are alike

@@ -89,7 +89,7 @@ __device__ __forceinline__ void wait_younger(int n) {
 // offsets do.
 template <bool A_F32, bool PACKED, int EPI, bool OUT_F32, class TL, int NJ, bool FAR>
 __device__ __forceinline__ void any_tile(const char* __restrict__ A, const char* __restrict__ W, void* __restrict__ Cout,
-                                         uint16_t* aux, size_t crow0, int rows_left, int n0, int Kdim, int Ndim,
+                                         AuxOf<EPI> aux, size_t crow0, int rows_left, int n0, int Kdim, int Ndim,
                                          uint32_t lds0, char* smem) {
   using S = AnyShape<A_F32, TL, NJ>;
   constexpr int BN = TL::BN;
@@ -213,9 +213,9 @@ __device__ __forceinline__ void any_tile(const char* __restrict__ A, const char*
 #pragma unroll
       for (int ni = 0; ni < NI; ++ni) {
         const int n = n0 + (2 * ni + wn) * 16 + kq * 4;  // a lane holds D[n .. n+3][m]
-        if (n < Ndim)  // Ndim % 8 == 0 and n % 4 == 0: the quad is entirely inside or outside
+        if (EPI == kEpiGeluSave8 || n < Ndim)  // Ndim % 8 == 0 and n % 4 == 0: the quad is entirely inside or outside
           store_quad<EPI, OUT_F32>(Cout, aux, crow0 + m, Ndim, n, acc[ni][j][0], acc[ni][j][1], acc[ni][j][2],
-                                   acc[ni][j][3]);
+                                   acc[ni][j][3], n < Ndim);
       }
     }
   }
@@ -246,7 +246,7 @@ __device__ __forceinline__ int wave_scan(int v) {
 // rows, 308 with up to 128.
 template <bool A_F32, bool PACKED, int EPI, bool OUT_F32, class TL, bool DEALT, bool FAR>
 __global__ __launch_bounds__(kAnyThreads, 2) void ffn_gemm_any(const char* __restrict__ A, const char* __restrict__ W,
-                                                               void* __restrict__ Cout, uint16_t* aux,
+                                                               void* __restrict__ Cout, AuxOf<EPI> aux,
                                                                const int32_t* __restrict__ seg_off,
                                                                const int32_t* __restrict__ buf_expert, int Kdim,
                                                                int Ndim, int NT, int E, int slots) {
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(kAnyThreads, 2) void ffn_gemm_any(const char* __res
 }
 
 template <bool A_F32, bool PACKED, int EPI, bool OUT_F32, class TL, bool DEALT, bool FAR>
-int launch_any(const void* A, const void* W, void* C, void* aux, const int32_t* seg_off, const int32_t* buf_expert, int E,
+int launch_any(const void* A, const void* W, void* C, AuxOf<EPI> aux, const int32_t* seg_off, const int32_t* buf_expert, int E,
                int rows_max, int T, int Kdim, int Ndim, hipStream_t st) {
   const int NT = ceil_div(Ndim, TL::BN);
   // m-tiles: at most those of full segments, and at most a partial one per segment beside those that T rows fill
@@ -344,7 +344,7 @@ int launch_any(const void* A, const void* W, void* C, void* aux, const int32_t* 
   static std::atomic<uint64_t> lds_allowed;
   if (!allow_lds((const void*)kern, kAnyLds, lds_allowed)) return LOCMOE_ERR_HIP;
   hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(kAnyThreads), kAnyLds, st, (const char*)A, (const char*)W, C,
-                     (uint16_t*)aux, seg_off, buf_expert, Kdim, Ndim, NT, E, cu_count() / 4);
+                     aux, seg_off, buf_expert, Kdim, Ndim, NT, E, cu_count() / 4);
   return launch_status();
 }
 
@@ -448,7 +448,7 @@ AnyTiles any_tiles(bool a_f32, bool packed, int E, int rows_max, int T, int Kdim
 }
 
 template <bool A_F32, bool PACKED, int EPI, bool OUT_F32>
-int any_gemm(const void* A, const void* W, void* C, void* aux, const int32_t* seg_off, const int32_t* buf_expert, int E,
+int any_gemm(const void* A, const void* W, void* C, AuxOf<EPI> aux, const int32_t* seg_off, const int32_t* buf_expert, int E,
              int rows_max, int T, int Kdim, int Ndim, hipStream_t st) {
   // (a limit of the interface, see the header; the grid has none that buffers of a card reach)
   if (!PACKED && (A_F32 || Kdim % 64 || Ndim % 256) && (long long)E * ceil_div(rows_max, 64) > 65535)
@@ -477,9 +477,9 @@ int any_gemm(const void* A, const void* W, void* C, void* aux, const int32_t* se
 #undef LOCMOE_ANY
 }
 
-#define LOCMOE_ANY_GEMM(...)                                                                                      \
-  template int any_gemm<__VA_ARGS__>(const void*, const void*, void*, void*, const int32_t*, const int32_t*, int, \
-                                     int, int, int, int, hipStream_t);
+#define LOCMOE_ANY_GEMM(A_F32, PACKED, EPI, OUT_F32)                                                                    \
+  template int any_gemm<A_F32, PACKED, EPI, OUT_F32>(const void*, const void*, void*, AuxOf<EPI>, const int32_t*,     \
+                                                     const int32_t*, int, int, int, int, int, hipStream_t);
 LOCMOE_ANY_GEMM(false, true, kEpiNone, false)
 LOCMOE_ANY_GEMM(false, true, kEpiGelu, false)
 LOCMOE_ANY_GEMM(false, false, kEpiNone, false)
@@ -492,4 +492,10 @@ LOCMOE_ANY_GEMM(false, false, kEpiNone, true)
 LOCMOE_ANY_GEMM(true, false, kEpiGelu, false)
 LOCMOE_ANY_GEMM(true, false, kEpiGeluSave, false)
 LOCMOE_ANY_GEMM(true, false, kEpiGeluGrad, false)
+LOCMOE_ANY_GEMM(false, true, kEpiGeluSave8, false)
+LOCMOE_ANY_GEMM(false, true, kEpiGeluGrad8, false)
+LOCMOE_ANY_GEMM(false, false, kEpiGeluSave8, false)
+LOCMOE_ANY_GEMM(false, false, kEpiGeluGrad8, false)
+LOCMOE_ANY_GEMM(true, false, kEpiGeluSave8, false)
+LOCMOE_ANY_GEMM(true, false, kEpiGeluGrad8, false)
 }  // namespace locmoe

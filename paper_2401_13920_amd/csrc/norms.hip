@@ -1,0 +1,606 @@
+// The norms of a transformer block around the layer, each in one pass with its neighbour in the path:
+//   locmoe_norm_gate          xn = x r gamma, r = 1 / sqrt(mean x^2 + eps), and Eq. 4's gating value of it
+//   locmoe_combine_norm       y = res + scale w gamma n, n = out[slot] r (or out[slot] itself): combine, norm, residual
+//   locmoe_combine_norm_bwd   its gradients: dout, dw, dgamma
+//   locmoe_dispatch_norm_bwd  dxn = dsend[slot] + (E/d) dg, and the norm's backward: dx, dgamma
+// Every row is read once, held in registers between the sum over it and its use, and written once.  LPR lanes share a row,
+// CPL 16-byte chunks each.  All of it is bound by memory.
+//
+// A column's gradient (dgamma) is a sum over tokens: a work-group sums its rows in registers, writes one row of partial
+// sums to the workspace, and a second kernel adds those in a fixed order: no atomics, the same bits every time.
+#include <math.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "common.h"
+
+namespace locmoe {
+namespace {
+
+constexpr int kNormThreads = 256;
+constexpr int kNormMaxParts = 1024;         // rows of partial sums at most
+constexpr int kNormMaxChunks = LOCMOE_NORM_MAX_ROW_BYTES / 16;
+constexpr int kMaxNormLds = kNormMaxChunks * 8 * 4;  // every feature of the longest row
+
+template <bool BF16>
+struct Vec {
+  static constexpr int N = BF16 ? 8 : 4;
+};
+
+template <bool BF16>
+__device__ __forceinline__ void unpack16(const uint4& v, float (&a)[Vec<BF16>::N]) {
+  const uint32_t* p = &v.x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (BF16) {
+      a[2 * i] = bf16_bits_to_f32(p[i] & 0xFFFFu);
+      a[2 * i + 1] = __uint_as_float(p[i] & 0xFFFF0000u);
+    } else {
+      a[i] = __uint_as_float(p[i]);
+    }
+  }
+}
+template <bool BF16>
+__device__ __forceinline__ uint4 pack16(const float (&a)[Vec<BF16>::N]) {
+  uint4 r;
+  uint32_t* p = &r.x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (BF16) p[i] = pack_bf16x2(a[2 * i], a[2 * i + 1]);
+    else p[i] = __float_as_uint(a[i]);
+  }
+  return r;
+}
+template <bool BF16>
+__device__ __forceinline__ float sumsq16(const uint4& v) {
+  return BF16 ? sumsq8_bf16(v) : sumsq4_f32(v);
+}
+// N floats of a vector over the columns (gamma); ones if there is none
+template <int N>
+__device__ __forceinline__ void load_cols(const float* p, int c, float (&a)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) {
+    const float4 v = p ? *(const float4*)(p + (size_t)c * N + i) : make_float4(1.f, 1.f, 1.f, 1.f);
+    a[i] = v.x; a[i + 1] = v.y; a[i + 2] = v.z; a[i + 3] = v.w;
+  }
+}
+
+template <int LPR>
+constexpr int threads_of() { return LPR > kNormThreads ? LPR : kNormThreads; }
+
+// The sum over a row's LPR lanes, in every one of them.  Rows of more than a wave go through LDS words of `sm`, which the
+// caller alternates between two sets (one barrier per sum).
+template <int LPR>
+__device__ __forceinline__ float row_sum(float v, float* sm) {
+  if constexpr (LPR <= kWave) {
+    return group_sum<LPR>(v);
+  } else {
+    constexpr int W = LPR / kWave;
+    v = group_sum<kWave>(v);
+    const int wave = threadIdx.x / kWave;
+    if (threadIdx.x % kWave == 0) sm[wave] = v;
+    __syncthreads();
+    const int w0 = wave / W * W;
+    float s = sm[w0];
+#pragma unroll
+    for (int i = 1; i < W; ++i) s += sm[w0 + i];
+    return s;
+  }
+}
+// sum over aligned groups of L lanes, L a power of two up to 64
+__device__ __forceinline__ float lanes_sum(float v, int L) {
+  if (L >= 2) v += dpp_f32<kDppXor1>(v);
+  if (L >= 4) v += dpp_f32<kDppXor2>(v);
+  if (L >= 8) v += dpp_f32<kDppHalfMirror>(v);
+  if (L >= 16) v += dpp_f32<kDppMirror>(v);
+  if (L >= 32) v += __shfl_xor(v, 16);
+  if (L >= 64) v += __shfl_xor(v, 32);
+  return v;
+}
+
+// How the means of the d/E features are formed: kLanes, a block is a power of two of chunks, held by neighbouring lanes of a
+// wave; kChunks, whole chunks, whose sums go through LDS; kElements, neither: every feature goes through LDS.
+enum GateForm { kLanes, kChunks, kElements };
+
+template <bool BF16, int LPR, int CPL, int GATE>
+__global__ __launch_bounds__(threads_of<LPR>()) void norm_gate_kernel(const uint4* __restrict__ x,
+                                                                      const float* __restrict__ gamma,
+                                                                      uint4* __restrict__ xn, float* __restrict__ rstd,
+                                                                      float* __restrict__ g, int T, int chunks, int E,
+                                                                      int blk, float inv_d, float eps) {
+  constexpr int V = Vec<BF16>::N, THREADS = threads_of<LPR>(), RPB = THREADS / LPR;
+  __shared__ float sm[THREADS / kWave];
+  extern __shared__ float part[];  // kChunks: [RPB][chunks], kElements: [RPB][chunks V]
+  const int rg = threadIdx.x / LPR, l = threadIdx.x % LPR;
+  const int m = blockIdx.x * RPB + rg;
+  const bool live = m < T;
+  const uint4* src = x + (size_t)(live ? m : T - 1) * chunks;
+  uint4 v[CPL];
+#pragma unroll
+  for (int i = 0; i < CPL; ++i) {
+    const int c = l + i * LPR;
+    v[i] = c < chunks ? nt_load16(src + c) : make_uint4(0, 0, 0, 0);
+  }
+  float ss = 0.f;
+#pragma unroll
+  for (int i = 0; i < CPL; ++i) ss += sumsq16<BF16>(v[i]);
+  const float r = 1.0f / sqrtf(row_sum<LPR>(ss, sm) * inv_d + eps);
+  const float inv_blk = 1.0f / (float)blk;
+  const int L = blk / V;  // (kLanes, kChunks)
+  if (live && l == 0 && rstd) rstd[m] = r;
+#pragma unroll
+  for (int i = 0; i < CPL; ++i) {
+    const int c = l + i * LPR;
+    const bool in = c < chunks;
+    float a[V], gm[V];
+    unpack16<BF16>(v[i], a);
+    load_cols<V>(gamma, in ? c : 0, gm);
+#pragma unroll
+    for (int k = 0; k < V; ++k) a[k] = a[k] * r * gm[k];
+    if (in && live) nt_store16(pack16<BF16>(a), xn + (size_t)m * chunks + c);
+    if (!g) continue;
+    if constexpr (GATE == kElements) {
+      if (in) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) part[((size_t)rg * chunks + c) * V + k] = a[k];
+      }
+    } else {
+      float s = (a[0] + a[1]) + (a[2] + a[3]);
+      if constexpr (V == 8) s += (a[4] + a[5]) + (a[6] + a[7]);
+      if constexpr (GATE == kLanes) {
+        s = lanes_sum(in ? s : 0.f, L);
+        if (in && live && (l & (L - 1)) == 0) g[(size_t)m * E + c / L] = s * inv_blk;
+      } else {
+        if (in) part[(size_t)rg * chunks + c] = s;
+      }
+    }
+  }
+  if constexpr (GATE != kLanes) {
+    if (!g) return;
+    __syncthreads();
+    // P lanes per output
+    const int n = GATE == kElements ? blk : L;
+    const float* row = part + (size_t)rg * chunks * (GATE == kElements ? V : 1);
+    int P = 1;
+    while (2 * P * E <= LPR && P < kWave && P < n) P *= 2;
+    for (int o0 = 0; o0 < E; o0 += LPR / P) {
+      const int o = o0 + l / P;
+      float s = 0.f;
+      if (o < E)
+        for (int k = l % P; k < n; k += P) s += row[o * n + k];
+      s = lanes_sum(s, P);
+      if (o < E && live && l % P == 0) g[(size_t)m * E + o] = s * inv_blk;
+    }
+  }
+}
+
+// POST: the norm behind the layer.  A dropped token's row is its residual, bit for bit.
+template <bool BF16, int LPR, int CPL, bool POST>
+__global__ __launch_bounds__(threads_of<LPR>()) void combine_norm_kernel(const uint4* __restrict__ out,
+                                                                         const int32_t* __restrict__ slot,
+                                                                         const float* __restrict__ w, const uint4* res,
+                                                                         const float* __restrict__ gamma, uint4* y,
+                                                                         float* __restrict__ rstd, int T, int chunks,
+                                                                         float inv_d, float eps, float scale) {
+  constexpr int V = Vec<BF16>::N, THREADS = threads_of<LPR>(), RPB = THREADS / LPR;
+  __shared__ float sm[THREADS / kWave];
+  const int rg = threadIdx.x / LPR, l = threadIdx.x % LPR;
+  const int m = blockIdx.x * RPB + rg;
+  const bool live = m < T;
+  const int s = live ? slot[m] : -1;
+  uint4 vo[CPL], vr[CPL];
+#pragma unroll
+  for (int i = 0; i < CPL; ++i) {
+    const int c = l + i * LPR;
+    vr[i] = live && c < chunks ? nt_load16(res + (size_t)m * chunks + c) : make_uint4(0, 0, 0, 0);
+  }
+#pragma unroll
+  for (int i = 0; i < CPL; ++i) {
+    const int c = l + i * LPR;
+    vo[i] = s >= 0 && c < chunks ? nt_load16(out + (size_t)s * chunks + c) : make_uint4(0, 0, 0, 0);
+  }
+  float r = 1.0f;
+  if (POST) {
+    float ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) ss += sumsq16<BF16>(vo[i]);
+    r = 1.0f / sqrtf(row_sum<LPR>(ss, sm) * inv_d + eps);
+  }
+  if (!live) return;
+  if (l == 0 && rstd) rstd[m] = s >= 0 ? r : 0.f;
+  const float f = s >= 0 ? scale * w[m] * r : 0.f;
+#pragma unroll
+  for (int i = 0; i < CPL; ++i) {
+    const int c = l + i * LPR;
+    if (c >= chunks) continue;
+    uint4 o = vr[i];
+    if (s >= 0) {
+      float a[V], b[V], gm[V];
+      unpack16<BF16>(vo[i], a);
+      unpack16<BF16>(vr[i], b);
+      load_cols<V>(gamma, c, gm);
+#pragma unroll
+      for (int k = 0; k < V; ++k) b[k] = fmaf(a[k] * f, gm[k], b[k]);
+      o = pack16<BF16>(b);
+    }
+    nt_store16(o, y + (size_t)m * chunks + c);
+  }
+}
+
+// The partial column sums of a work-group's rows -> row blockIdx.x of `part`.  Row groups are added in order through LDS.
+template <int LPR, int CPL, int V>
+__device__ __forceinline__ void store_partial(const float (&acc)[CPL][V], float* part, int chunks, float* lds) {
+  constexpr int RPB = threads_of<LPR>() / LPR;
+  const int rg = threadIdx.x / LPR, l = threadIdx.x % LPR;
+  float* dst = part + (size_t)blockIdx.x * chunks * V;
+  if constexpr (RPB > 1) {
+#pragma unroll
+    for (int i = 0; i < CPL; ++i)
+#pragma unroll
+      for (int k = 0; k < V; k += 4)
+        *(float4*)(lds + ((rg * CPL + i) * LPR + l) * V + k) =
+            make_float4(acc[i][k], acc[i][k + 1], acc[i][k + 2], acc[i][k + 3]);
+    __syncthreads();
+    for (int q = threadIdx.x; q < CPL * LPR * V; q += threads_of<LPR>()) {
+      float s = lds[q];
+      for (int j = 1; j < RPB; ++j) s += lds[j * CPL * LPR * V + q];
+      if (q < chunks * V) dst[q] = s;  // (chunk l + i LPR, value k: the column order)
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) {
+      const int c = l + i * LPR;
+      if (c < chunks) {
+#pragma unroll
+        for (int k = 0; k < V; k += 4)
+          *(float4*)(dst + (size_t)c * V + k) = make_float4(acc[i][k], acc[i][k + 1], acc[i][k + 2], acc[i][k + 3]);
+      }
+    }
+  }
+}
+
+// With n the row that the forward multiplied (out r, or out without the norm) and u = scale gamma dy:
+//   dw = <u, n>,   dgamma += scale w dy n,   dout = r w (u - n dw / d), or w u without the norm.
+template <bool BF16, int LPR, int CPL, bool POST>
+__global__ __launch_bounds__(threads_of<LPR>()) void combine_norm_bwd_kernel(
+    const uint4* __restrict__ dy, const uint4* __restrict__ out, const int32_t* __restrict__ slot,
+    const float* __restrict__ w, const float* __restrict__ gamma, const float* __restrict__ rstd, uint4* __restrict__ dout,
+    float* __restrict__ dw, float* __restrict__ part, int T, int chunks, float inv_d, float scale) {
+  constexpr int V = Vec<BF16>::N, THREADS = threads_of<LPR>(), RPB = THREADS / LPR;
+  __shared__ float sm[2][THREADS / kWave];
+  __shared__ float lds[RPB > 1 ? THREADS * CPL * V : 1];
+  const int rg = threadIdx.x / LPR, l = threadIdx.x % LPR;
+  float gm[CPL][V], acc[CPL][V];
+#pragma unroll
+  for (int i = 0; i < CPL; ++i) {
+    const int c = l + i * LPR;
+    load_cols<V>(gamma, c < chunks ? c : 0, gm[i]);
+#pragma unroll
+    for (int k = 0; k < V; ++k) { gm[i][k] *= scale; acc[i][k] = 0.f; }
+  }
+  int set = 0;
+  for (int m0 = blockIdx.x * RPB; m0 < T; m0 += gridDim.x * RPB, set ^= 1) {
+    const int m = m0 + rg;
+    const int s = m < T ? slot[m] : -1;
+    const float wm = s >= 0 ? w[m] : 0.f, r = POST ? (s >= 0 ? rstd[m] : 0.f) : 1.f;
+    uint4 vd[CPL], vo[CPL];
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) {
+      const int c = l + i * LPR;
+      const bool in = s >= 0 && c < chunks;
+      vd[i] = in ? nt_load16(dy + (size_t)m * chunks + c) : make_uint4(0, 0, 0, 0);
+      vo[i] = in ? nt_load16(out + (size_t)s * chunks + c) : make_uint4(0, 0, 0, 0);
+    }
+    const float ws = wm * scale;
+    float dot = 0.f;
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) {
+      float a[V], b[V];
+      unpack16<BF16>(vd[i], a);
+      unpack16<BF16>(vo[i], b);
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float n = b[k] * r;
+        dot = fmaf(a[k] * gm[i][k], n, dot);
+        acc[i][k] = fmaf(a[k] * ws, n, acc[i][k]);
+      }
+    }
+    dot = row_sum<LPR>(dot, sm[set]);
+    if (m < T && l == 0) dw[m] = dot;
+    if (s < 0) continue;
+    const float mean = POST ? dot * inv_d : 0.f, wr = wm * r;
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) {
+      const int c = l + i * LPR;
+      if (c >= chunks) continue;
+      float a[V], b[V];
+      unpack16<BF16>(vd[i], a);
+      unpack16<BF16>(vo[i], b);
+#pragma unroll
+      for (int k = 0; k < V; ++k) a[k] = wr * (POST ? fmaf(-mean, b[k] * r, a[k] * gm[i][k]) : a[k] * gm[i][k]);
+      nt_store16(pack16<BF16>(a), dout + (size_t)s * chunks + c);
+    }
+  }
+  if (part) store_partial<LPR, CPL, V>(acc, part, chunks, lds);
+}
+
+// VEC_BLOCK: a chunk lies inside one GrAP block.  With xh = x r, dh = dxn gamma:
+//   dgamma += dxn xh,   dx = dres + r (dh - xh mean(dh xh)).
+template <bool BF16, int LPR, int CPL, bool VEC_BLOCK>
+__global__ __launch_bounds__(threads_of<LPR>()) void dispatch_norm_bwd_kernel(
+    const uint4* __restrict__ dsend, const int32_t* __restrict__ slot, const float* __restrict__ dg,
+    const uint4* __restrict__ x, const float* __restrict__ gamma, const float* __restrict__ rstd, const uint4* dres,
+    uint4* dx, float* __restrict__ part, int T, int chunks, int E, int blk, float inv_d, float dg_scale) {
+  constexpr int V = Vec<BF16>::N, THREADS = threads_of<LPR>(), RPB = THREADS / LPR;
+  __shared__ float sm[2][THREADS / kWave];
+  __shared__ float lds[RPB > 1 ? THREADS * CPL * V : 1];
+  const int rg = threadIdx.x / LPR, l = threadIdx.x % LPR;
+  float gm[CPL][V], acc[CPL][V];
+#pragma unroll
+  for (int i = 0; i < CPL; ++i) {
+    const int c = l + i * LPR;
+    load_cols<V>(gamma, c < chunks ? c : 0, gm[i]);
+#pragma unroll
+    for (int k = 0; k < V; ++k) acc[i][k] = 0.f;
+  }
+  int set = 0;
+  for (int m0 = blockIdx.x * RPB; m0 < T; m0 += gridDim.x * RPB, set ^= 1) {
+    const int m = m0 + rg;
+    const bool live = m < T;
+    const int s = live ? slot[m] : -1;
+    const float r = live ? rstd[m] : 0.f;
+    uint4 vs[CPL], vx[CPL], vr[CPL];
+    float t[CPL][VEC_BLOCK ? 1 : V];
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) {
+      const int c = l + i * LPR;
+      const bool in = live && c < chunks;
+      vs[i] = in && s >= 0 ? nt_load16(dsend + (size_t)s * chunks + c) : make_uint4(0, 0, 0, 0);
+      vx[i] = in ? nt_load16(x + (size_t)m * chunks + c) : make_uint4(0, 0, 0, 0);
+      vr[i] = in && dres ? nt_load16(dres + (size_t)m * chunks + c) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int k = 0; k < (VEC_BLOCK ? 1 : V); ++k) t[i][k] = in ? dg_scale * dg[(size_t)m * E + (c * V + k) / blk] : 0.f;
+    }
+    float dot = 0.f;
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) {
+      float a[V], b[V];
+      unpack16<BF16>(vs[i], a);
+      unpack16<BF16>(vx[i], b);
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float dxn = a[k] + t[i][VEC_BLOCK ? 0 : k], p = dxn * (b[k] * r);
+        acc[i][k] += p;
+        dot = fmaf(p, gm[i][k], dot);
+      }
+    }
+    const float mean = row_sum<LPR>(dot, sm[set]) * inv_d;
+    if (!live) continue;
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) {
+      const int c = l + i * LPR;
+      if (c >= chunks) continue;
+      float a[V], b[V], q[V];
+      unpack16<BF16>(vs[i], a);
+      unpack16<BF16>(vx[i], b);
+      unpack16<BF16>(vr[i], q);
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        a[k] = fmaf(r, fmaf(a[k] + t[i][VEC_BLOCK ? 0 : k], gm[i][k], -(b[k] * r) * mean), q[k]);
+      nt_store16(pack16<BF16>(a), dx + (size_t)m * chunks + c);
+    }
+  }
+  if (part) store_partial<LPR, CPL, V>(acc, part, chunks, lds);
+}
+
+// dgamma[j] = sum of column j over the rows of partial sums.  A work-group makes 64 columns: 16 lanes of four columns, 16 row
+// groups, which are added in order through LDS.
+__global__ __launch_bounds__(256) void column_sum_kernel(const float* __restrict__ part, float* __restrict__ dgamma,
+                                                         int rows, int d) {
+  __shared__ float4 s[16][16];
+  const int j = threadIdx.x & 15, rg = threadIdx.x >> 4, col = blockIdx.x * 64 + j * 4;
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (col < d) {
+    constexpr int U = 8;
+    for (int q0 = rg; q0 < rows; q0 += 16 * U) {
+      float4 v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = *(const float4*)(part + (size_t)min(q0 + 16 * u, rows - 1) * d + col);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (q0 + 16 * u < rows) { a.x += v[u].x; a.y += v[u].y; a.z += v[u].z; a.w += v[u].w; }
+    }
+  }
+  s[rg][j] = a;
+  __syncthreads();
+  if (rg == 0 && col < d) {
+    for (int i = 1; i < 16; ++i) { const float4 v = s[i][j]; a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w; }
+    *(float4*)(dgamma + col) = a;
+  }
+}
+
+// The lanes of a row of `chunks` chunks: f(RowShape<lanes, chunks a lane>).  Forward rows are held by a wave or less where eight
+// chunks a lane suffice (no barrier); backward rows, which carry gamma and its gradient in registers too, by more lanes.
+template <int LPR_, int CPL_>
+struct RowShape { static constexpr int LPR = LPR_, CPL = CPL_, kThreads = threads_of<LPR_>(), kRows = kThreads / LPR_; };
+template <class F>
+int with_forward_row(int chunks, F&& f) {
+  if (chunks <= 16) return f(RowShape<16, 1>{});
+  if (chunks <= 32) return f(RowShape<16, 2>{});
+  if (chunks <= 64) return f(RowShape<64, 1>{});
+  if (chunks <= 128) return f(RowShape<64, 2>{});
+  if (chunks <= 256) return f(RowShape<64, 4>{});
+  if (chunks <= 512) return f(RowShape<64, 8>{});
+  if (chunks <= 1024) return f(RowShape<256, 4>{});
+  if (chunks <= 2048) return f(RowShape<512, 4>{});
+  return f(RowShape<1024, 4>{});
+}
+template <class F>
+int with_backward_row(int chunks, F&& f) {
+  if (chunks <= 16) return f(RowShape<16, 1>{});
+  if (chunks <= 64) return f(RowShape<64, 1>{});
+  if (chunks <= 128) return f(RowShape<64, 2>{});
+  if (chunks <= 256) return f(RowShape<256, 1>{});
+  if (chunks <= 512) return f(RowShape<256, 2>{});
+  if (chunks <= 1024) return f(RowShape<512, 2>{});
+  if (chunks <= 2048) return f(RowShape<1024, 2>{});
+  return f(RowShape<1024, 4>{});
+}
+
+// What the four entry points share: the row in 16-byte chunks
+struct NormRow {
+  bool bf;
+  int chunks, blk;
+  float inv_d;
+};
+int norm_row(const locmoe_desc* p, NormRow* r) {
+  const int st = check_desc(p);
+  if (st != LOCMOE_OK) return st;
+  r->bf = p->x_dtype == LOCMOE_BF16;
+  r->chunks = p->d / (r->bf ? 8 : 4);
+  r->blk = p->d / p->E;
+  r->inv_d = 1.0f / (float)p->d;
+  return r->chunks > kNormMaxChunks ? LOCMOE_ERR_SHAPE : LOCMOE_OK;
+}
+inline bool finite(float v) { return v - v == 0.0f; }
+
+inline int part_rows(int T, int rows_per_group) { return std::min(ceil_div(T, rows_per_group), kNormMaxParts); }
+
+template <bool BF>
+int norm_gate_impl(const NormRow& row, const locmoe_desc* desc, const void* x, const float* gamma, float eps, void* xn,
+                   float* rstd, float* g, hipStream_t s) {
+  const int T = desc->T, E = desc->E, V = Vec<BF>::N, L = row.blk / V;
+  return with_forward_row(row.chunks, [&](auto shape) {
+    using S = decltype(shape);
+    const GateForm form = row.blk % V ? kElements : (L & (L - 1)) == 0 && L <= std::min(S::LPR, kWave) ? kLanes : kChunks;
+    const size_t lds = !g || form == kLanes ? 0 : (size_t)S::kRows * row.chunks * (form == kElements ? V : 1) * 4;
+    auto kern = form == kLanes    ? norm_gate_kernel<BF, S::LPR, S::CPL, kLanes>
+                : form == kChunks ? norm_gate_kernel<BF, S::LPR, S::CPL, kChunks>
+                                  : norm_gate_kernel<BF, S::LPR, S::CPL, kElements>;
+    static std::atomic<uint64_t> allowed[3];
+    // (the limit without asking is 64 KiB, some of which are the kernel's own words)
+    if (lds > 60000 && !allow_lds((const void*)kern, kMaxNormLds, allowed[form])) return (int)LOCMOE_ERR_HIP;
+    hipLaunchKernelGGL(kern, dim3(ceil_div(T, S::kRows)), dim3(S::kThreads), lds, s, (const uint4*)x, gamma, (uint4*)xn, rstd,
+                       g, T, row.chunks, E, row.blk, row.inv_d, eps);
+    return launch_status();
+  });
+}
+
+template <bool BF>
+int combine_norm_impl(const NormRow& row, int T, const void* out, const int32_t* slot, const float* w, const void* res,
+                      const float* gamma, bool post, float eps, float scale, void* y, float* rstd, hipStream_t s) {
+  return with_forward_row(row.chunks, [&](auto shape) {
+    using S = decltype(shape);
+    auto kern = post ? combine_norm_kernel<BF, S::LPR, S::CPL, true> : combine_norm_kernel<BF, S::LPR, S::CPL, false>;
+    hipLaunchKernelGGL(kern, dim3(ceil_div(T, S::kRows)), dim3(S::kThreads), 0, s, (const uint4*)out, slot, w,
+                       (const uint4*)res, gamma, (uint4*)y, rstd, T, row.chunks, row.inv_d, eps, scale);
+    return launch_status();
+  });
+}
+
+void sum_columns(const float* part, float* dgamma, int rows, int d, hipStream_t s) {
+  if (dgamma) hipLaunchKernelGGL(column_sum_kernel, dim3(ceil_div(d, 64)), dim3(256), 0, s, part, dgamma, rows, d);
+}
+
+template <bool BF>
+int combine_norm_bwd_impl(const NormRow& row, const locmoe_desc* desc, const void* dy, const void* out, const int32_t* slot,
+                          const float* w, const float* gamma, bool post, float scale, const float* rstd, void* dout,
+                          float* dw, float* dgamma, void* ws, hipStream_t s) {
+  return with_backward_row(row.chunks, [&](auto shape) {
+    using S = decltype(shape);
+    const int rows = part_rows(desc->T, S::kRows);
+    float* part = dgamma ? (float*)ws : nullptr;
+    auto kern = post ? combine_norm_bwd_kernel<BF, S::LPR, S::CPL, true> : combine_norm_bwd_kernel<BF, S::LPR, S::CPL, false>;
+    hipLaunchKernelGGL(kern, dim3(rows), dim3(S::kThreads), 0, s, (const uint4*)dy, (const uint4*)out, slot, w, gamma, rstd,
+                       (uint4*)dout, dw, part, desc->T, row.chunks, row.inv_d, scale);
+    sum_columns(part, dgamma, rows, desc->d, s);
+    return launch_status();
+  });
+}
+
+template <bool BF>
+int dispatch_norm_bwd_impl(const NormRow& row, const locmoe_desc* desc, const void* dsend, const int32_t* slot,
+                           const float* dg, const void* x, const float* gamma, const float* rstd, const void* dres, void* dx,
+                           float* dgamma, void* ws, hipStream_t s) {
+  return with_backward_row(row.chunks, [&](auto shape) {
+    using S = decltype(shape);
+    const int rows = part_rows(desc->T, S::kRows);
+    float* part = dgamma ? (float*)ws : nullptr;
+    auto kern = row.blk % Vec<BF>::N == 0 ? dispatch_norm_bwd_kernel<BF, S::LPR, S::CPL, true>
+                                          : dispatch_norm_bwd_kernel<BF, S::LPR, S::CPL, false>;
+    hipLaunchKernelGGL(kern, dim3(rows), dim3(S::kThreads), 0, s, (const uint4*)dsend, slot, dg, (const uint4*)x, gamma, rstd,
+                       (const uint4*)dres, (uint4*)dx, part, desc->T, row.chunks, desc->E, row.blk, row.inv_d,
+                       (float)desc->E / (float)desc->d);
+    sum_columns(part, dgamma, rows, desc->d, s);
+    return launch_status();
+  });
+}
+
+inline bool norm_ws_ok(const locmoe_desc* desc, const float* dgamma, const void* ws, size_t ws_bytes) {
+  return !dgamma || (ws && ws_bytes >= locmoe_norm_workspace_bytes(desc));
+}
+
+}  // namespace
+}  // namespace locmoe
+
+extern "C" size_t locmoe_norm_workspace_bytes(const locmoe_desc* desc) {
+  using namespace locmoe;
+  NormRow row;
+  if (norm_row(desc, &row) != LOCMOE_OK) return 0;
+  return (size_t)std::min(desc->T, kNormMaxParts) * (size_t)desc->d * 4;
+}
+
+extern "C" int locmoe_norm_gate(const locmoe_desc* desc, const void* x, const float* gamma, float norm_eps, void* xn,
+                                float* rstd, float* g, void* stream) {
+  using namespace locmoe;
+  if (!desc || !x || !xn) return LOCMOE_ERR_NULL;
+  NormRow row;
+  const int st = norm_row(desc, &row);
+  if (st != LOCMOE_OK) return st;
+  if (!(norm_eps > 0.0f) || !finite(norm_eps)) return LOCMOE_ERR_ARG;
+  return row.bf ? norm_gate_impl<true>(row, desc, x, gamma, norm_eps, xn, rstd, g, as_stream(stream))
+                : norm_gate_impl<false>(row, desc, x, gamma, norm_eps, xn, rstd, g, as_stream(stream));
+}
+
+extern "C" int locmoe_combine_norm(const locmoe_desc* desc, const void* out, const int32_t* slot, const float* w,
+                                   const void* res, const float* gamma, int32_t post_norm, float norm_eps, float scale,
+                                   void* y, float* rstd, void* stream) {
+  using namespace locmoe;
+  if (!desc || !out || !slot || !w || !res || !y) return LOCMOE_ERR_NULL;
+  NormRow row;
+  const int st = norm_row(desc, &row);
+  if (st != LOCMOE_OK) return st;
+  if ((post_norm != 0 && post_norm != 1) || !finite(scale)) return LOCMOE_ERR_ARG;
+  if (post_norm && (!(norm_eps > 0.0f) || !finite(norm_eps))) return LOCMOE_ERR_ARG;
+  auto impl = row.bf ? combine_norm_impl<true> : combine_norm_impl<false>;
+  return impl(row, desc->T, out, slot, w, res, gamma, post_norm, norm_eps, scale, y, rstd, as_stream(stream));
+}
+
+extern "C" int locmoe_combine_norm_bwd(const locmoe_desc* desc, const void* dy, const void* out, const int32_t* slot,
+                                       const float* w, const float* gamma, int32_t post_norm, float scale,
+                                       const float* rstd, void* dout, float* dw, float* dgamma, void* ws,
+                                       size_t ws_bytes, void* stream) {
+  using namespace locmoe;
+  if (!desc || !dy || !out || !slot || !w || !dout || !dw || (post_norm && !rstd)) return LOCMOE_ERR_NULL;
+  NormRow row;
+  const int st = norm_row(desc, &row);
+  if (st != LOCMOE_OK) return st;
+  if ((post_norm != 0 && post_norm != 1) || !finite(scale)) return LOCMOE_ERR_ARG;
+  if (!norm_ws_ok(desc, dgamma, ws, ws_bytes)) return LOCMOE_ERR_WORKSPACE;
+  auto impl = row.bf ? combine_norm_bwd_impl<true> : combine_norm_bwd_impl<false>;
+  return impl(row, desc, dy, out, slot, w, gamma, post_norm, scale, rstd, dout, dw, dgamma, ws, as_stream(stream));
+}
+
+extern "C" int locmoe_dispatch_norm_bwd(const locmoe_desc* desc, const void* dsend, const int32_t* slot, const float* dg,
+                                        const void* x, const float* gamma, const float* rstd, const void* dres, void* dx,
+                                        float* dgamma, void* ws, size_t ws_bytes, void* stream) {
+  using namespace locmoe;
+  if (!desc || !dsend || !slot || !dg || !x || !rstd || !dx) return LOCMOE_ERR_NULL;
+  NormRow row;
+  const int st = norm_row(desc, &row);
+  if (st != LOCMOE_OK) return st;
+  if (!norm_ws_ok(desc, dgamma, ws, ws_bytes)) return LOCMOE_ERR_WORKSPACE;
+  auto impl = row.bf ? dispatch_norm_bwd_impl<true> : dispatch_norm_bwd_impl<false>;
+  return impl(row, desc, dsend, slot, dg, x, gamma, rstd, dres, dx, dgamma, ws, as_stream(stream));
+}

@@ -27,8 +27,14 @@ EXPORTS = ("locmoe_status_string", "locmoe_capacity_min", "locmoe_p_delta", "loc
            "locmoe_dispatch_bwd", "locmoe_expert_ffn_in_save", "locmoe_transpose_weights",
            "locmoe_expert_ffn_dgrad", "locmoe_expert_ffn_wgrad", "locmoe_pack_weights_t",
            "locmoe_expert_ffn_ws", "locmoe_expert_ffn_in_ws", "locmoe_expert_ffn_out_ws",
-           "locmoe_expert_ffn_in_save_ws", "locmoe_expert_ffn_dgrad_ws", "locmoe_gate_dense", "locmoe_route_hash")
+           "locmoe_expert_ffn_in_save_ws", "locmoe_expert_ffn_dgrad_ws", "locmoe_gate_dense", "locmoe_route_hash",
+           "locmoe_norm_workspace_bytes", "locmoe_norm_gate", "locmoe_combine_norm", "locmoe_combine_norm_bwd",
+           "locmoe_dispatch_norm_bwd", "locmoe_layer_few_workspace_bytes", "locmoe_layer_few",
+           "locmoe_expert_ffn_in_save8", "locmoe_expert_ffn_dgrad8", "locmoe_expert_ffn_in_save8_ws",
+           "locmoe_expert_ffn_dgrad8_ws")
 LOCMOE_FFN_WS_BYTES = 128
+LOCMOE_NORM_MAX_ROW_BYTES = 65536
+LOCMOE_FEW_MAX_TOKENS = 64
 LOCMOE_DISPATCH_STATIC_MAX_COUNTS = 262144
 
 
@@ -99,8 +105,23 @@ def lib() -> C.CDLL:
     L.locmoe_packed_weights_bytes.restype = SZ
     L.locmoe_packed_weights_bytes.argtypes = [D]
     L.locmoe_pack_weights.argtypes = [D] + [P] * 5
+    L.locmoe_norm_workspace_bytes.restype = SZ
+    L.locmoe_norm_workspace_bytes.argtypes = [D]
+    L.locmoe_layer_few_workspace_bytes.restype = SZ
+    L.locmoe_layer_few_workspace_bytes.argtypes = [D]
+    FLT = C.c_float
+    L.locmoe_norm_gate.argtypes = [D, P, P, FLT] + [P] * 4
+    L.locmoe_combine_norm.argtypes = [D] + [P] * 5 + [I32, FLT, FLT] + [P] * 3
+    L.locmoe_combine_norm_bwd.argtypes = [D] + [P] * 5 + [I32, FLT] + [P] * 5 + [SZ, P]
+    L.locmoe_dispatch_norm_bwd.argtypes = [D] + [P] * 10 + [SZ, P]
+    L.locmoe_layer_few.argtypes = [D] + [P] * 5 + [I32] + [P] * 5 + [SZ, P]
+    L.locmoe_expert_ffn_in_save8.argtypes = [D] + [P] * 8
+    L.locmoe_expert_ffn_dgrad8.argtypes = [D] + [P] * 11
+    L.locmoe_expert_ffn_in_save8_ws.argtypes = [D] + [P] * 8 + [SZ, P]
+    L.locmoe_expert_ffn_dgrad8_ws.argtypes = [D] + [P] * 11 + [SZ, P]
     for n in EXPORTS:
-        if n not in ("locmoe_status_string", "locmoe_workspace_bytes", "locmoe_packed_weights_bytes"):
+        if n not in ("locmoe_status_string", "locmoe_workspace_bytes", "locmoe_packed_weights_bytes",
+                     "locmoe_norm_workspace_bytes", "locmoe_layer_few_workspace_bytes"):
             getattr(L, n).restype = C.c_int
     L.locmoe_internal_ffn_kernel.restype = C.c_char_p
     L.locmoe_internal_ffn_kernel.argtypes = [D, C.c_int, C.c_int]
@@ -322,6 +343,66 @@ def locmoe_expert_ffn_wgrad(desc, send, H, dout, dZ, seg_off, buf_expert, dW_in,
                                          _ptr(buf_expert), _ptr(dW_in), _ptr(dW_out), _stream(stream)))
 
 
+# ---- the layer in a transformer block ----------------------------------------------------------
+def locmoe_norm_workspace_bytes(desc: locmoe_desc) -> int:
+    return int(lib().locmoe_norm_workspace_bytes(C.byref(desc)))
+
+
+def locmoe_norm_gate(desc, x, gamma, norm_eps, xn, rstd, g, stream=None):
+    _check(lib().locmoe_norm_gate(C.byref(desc), _ptr(x), _ptr(gamma), norm_eps, _ptr(xn), _ptr(rstd), _ptr(g),
+                                  _stream(stream)))
+
+
+def locmoe_combine_norm(desc, out, slot, w, res, gamma, post_norm, norm_eps, scale, y, rstd, stream=None):
+    _check(lib().locmoe_combine_norm(C.byref(desc), _ptr(out), _ptr(slot), _ptr(w), _ptr(res), _ptr(gamma),
+                                     int(post_norm), norm_eps, scale, _ptr(y), _ptr(rstd), _stream(stream)))
+
+
+def locmoe_combine_norm_bwd(desc, dy, out, slot, w, gamma, post_norm, scale, rstd, dout, dw, dgamma, ws, ws_bytes,
+                            stream=None):
+    _check(lib().locmoe_combine_norm_bwd(C.byref(desc), _ptr(dy), _ptr(out), _ptr(slot), _ptr(w), _ptr(gamma),
+                                         int(post_norm), scale, _ptr(rstd), _ptr(dout), _ptr(dw), _ptr(dgamma),
+                                         _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def locmoe_dispatch_norm_bwd(desc, dsend, slot, dg, x, gamma, rstd, dres, dx, dgamma, ws, ws_bytes, stream=None):
+    _check(lib().locmoe_dispatch_norm_bwd(C.byref(desc), _ptr(dsend), _ptr(slot), _ptr(dg), _ptr(x), _ptr(gamma),
+                                          _ptr(rstd), _ptr(dres), _ptr(dx), _ptr(dgamma), _ptr(ws), ws_bytes,
+                                          _stream(stream)))
+
+
+def locmoe_layer_few_workspace_bytes(desc: locmoe_desc) -> int:
+    return int(lib().locmoe_layer_few_workspace_bytes(C.byref(desc)))
+
+
+def locmoe_layer_few(desc, x, g, eps, W_in, W_out, weighted, eid, w, slot, y, ws, ws_bytes, stream=None):
+    _check(lib().locmoe_layer_few(C.byref(desc), _ptr(x), _ptr(g), _ptr(eps), _ptr(W_in), _ptr(W_out), int(weighted),
+                                  _ptr(eid), _ptr(w), _ptr(slot), _ptr(y), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def locmoe_expert_ffn_in_save8(desc, send, seg_off, buf_expert, W_in, H_ws, Zq, Zs, stream=None):
+    _check(lib().locmoe_expert_ffn_in_save8(C.byref(desc), _ptr(send), _ptr(seg_off), _ptr(buf_expert), _ptr(W_in),
+                                            _ptr(H_ws), _ptr(Zq), _ptr(Zs), _stream(stream)))
+
+
+def locmoe_expert_ffn_in_save8_ws(desc, send, seg_off, buf_expert, W_in, H_ws, Zq, Zs, ws, ws_bytes, stream=None):
+    _check(lib().locmoe_expert_ffn_in_save8_ws(C.byref(desc), _ptr(send), _ptr(seg_off), _ptr(buf_expert), _ptr(W_in),
+                                               _ptr(H_ws), _ptr(Zq), _ptr(Zs), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def locmoe_expert_ffn_dgrad8(desc, dout, Zq, Zs, seg_off, buf_expert, W_out_t, W_in_t, dZ, H_ws, dsend, stream=None):
+    _check(lib().locmoe_expert_ffn_dgrad8(C.byref(desc), _ptr(dout), _ptr(Zq), _ptr(Zs), _ptr(seg_off),
+                                          _ptr(buf_expert), _ptr(W_out_t), _ptr(W_in_t), _ptr(dZ), _ptr(H_ws),
+                                          _ptr(dsend), _stream(stream)))
+
+
+def locmoe_expert_ffn_dgrad8_ws(desc, dout, Zq, Zs, seg_off, buf_expert, W_out_t, W_in_t, dZ, H_ws, dsend, ws, ws_bytes,
+                                stream=None):
+    _check(lib().locmoe_expert_ffn_dgrad8_ws(C.byref(desc), _ptr(dout), _ptr(Zq), _ptr(Zs), _ptr(seg_off),
+                                             _ptr(buf_expert), _ptr(W_out_t), _ptr(W_in_t), _ptr(dZ), _ptr(H_ws),
+                                             _ptr(dsend), _ptr(ws), ws_bytes, _stream(stream)))
+
+
 # ---- buffer bundle: device allocations for one layer call (plumbing only) ---------------------
 @dataclass
 class Buffers:
@@ -403,7 +484,8 @@ class GradBuffers:
     dW_out: object
 
 
-def alloc_grad_buffers(desc: locmoe_desc, device="cuda") -> GradBuffers:
+def alloc_grad_buffers(desc: locmoe_desc, device="cuda", keep_z: bool = True) -> GradBuffers:
+    """`keep_z` False: no Z, for steps that keep the hidden activations in 8 bits (alloc_checkpoint8)."""
     import torch
     T, d, E, h, Cap = desc.T, desc.d, desc.E, desc.h, desc.C
     xd = torch.bfloat16 if desc.x_dtype == LOCMOE_BF16 else torch.float32
@@ -411,33 +493,166 @@ def alloc_grad_buffers(desc: locmoe_desc, device="cuda") -> GradBuffers:
     bf = dict(dtype=torch.bfloat16, device=device)
     f32 = dict(dtype=torch.float32, device=device)
     return GradBuffers(
-        Z=torch.empty(rows, h, **bf), dout=torch.empty(rows, d, dtype=xd, device=device), dw=torch.empty(T, **f32),
+        Z=torch.empty(rows, h, **bf) if keep_z else None, dout=torch.empty(rows, d, dtype=xd, device=device), dw=torch.empty(T, **f32),
         dZ=torch.empty(rows, h, **bf), dsend=torch.empty(rows, d, dtype=xd, device=device),
         coef=torch.empty(E, **f32), dg=torch.empty(T, E, **f32), dx=torch.empty(T, d, dtype=xd, device=device),
         dW_in=torch.empty(E, h, d, **bf), dW_out=torch.empty(E, d, h, **bf))
 
 
-def forward_train(desc, x, home, e2n, W_in, W_out, b: Buffers, gb: GradBuffers, eps=None, stream=None):
-    """The forward path with the pre-activation Z kept for the backward."""
+@dataclass
+class Checkpoint8:
+    """The hidden activations of one layer between its forward and its backward, 9 bits a value in place of Z and H: with one
+    for each layer, all layers can share the H of Buffers and the rest of GradBuffers."""
+    Zq: object
+    Zs: object
+
+
+def alloc_checkpoint8(desc: locmoe_desc, device="cuda") -> Checkpoint8:
+    import torch
+    rows = desc.E * desc.C
+    return Checkpoint8(Zq=torch.empty(rows, desc.h, dtype=torch.int8, device=device),
+                       Zs=torch.empty(rows, -(-desc.h // 16), dtype=torch.bfloat16, device=device))
+
+
+def _experts_train(desc, send, seg_off, buf_expert, W_in, W_out, b, gb, ckpt, stream):
+    """The expert FFN with the pre-activation kept, in bf16 (gb.Z) or in 8 bits (ckpt); returns out's address."""
+    H, out, ffn_ws = _ptr(b.H), _ptr(b.out), _ptr(b.ffn_ws)
+    if ckpt is None:
+        locmoe_expert_ffn_in_save_ws(desc, send, seg_off, buf_expert, W_in, H, gb.Z, ffn_ws, LOCMOE_FFN_WS_BYTES, stream)
+    else:
+        locmoe_expert_ffn_in_save8_ws(desc, send, seg_off, buf_expert, W_in, H, ckpt.Zq, ckpt.Zs, ffn_ws,
+                                      LOCMOE_FFN_WS_BYTES, stream)
+    locmoe_expert_ffn_out_ws(desc, H, seg_off, buf_expert, W_out, out, ffn_ws, LOCMOE_FFN_WS_BYTES, stream)
+    return out
+
+
+def _experts_backward(desc, dout, seg_off, buf_expert, W_in_t, W_out_t, b, gb, ckpt, stream):
+    """Data and weight gradients of the expert FFN; returns dsend's address."""
+    dZ, dsend, H = _ptr(gb.dZ), _ptr(gb.dsend), _ptr(b.H)
+    if ckpt is None:
+        locmoe_expert_ffn_dgrad_ws(desc, dout, gb.Z, seg_off, buf_expert, W_out_t, W_in_t, dZ, dsend, b.ffn_ws,
+                                   LOCMOE_FFN_WS_BYTES, stream)
+    else:
+        locmoe_expert_ffn_dgrad8_ws(desc, dout, ckpt.Zq, ckpt.Zs, seg_off, buf_expert, W_out_t, W_in_t, dZ, H, dsend,
+                                    b.ffn_ws, LOCMOE_FFN_WS_BYTES, stream)
+    locmoe_expert_ffn_wgrad(desc, b.send, H, dout, dZ, seg_off, buf_expert, gb.dW_in, gb.dW_out, stream)
+    return dsend
+
+
+def forward_train(desc, x, home, e2n, W_in, W_out, b: Buffers, gb: GradBuffers, eps=None, stream=None, ckpt=None):
+    """The forward path with the pre-activation kept for the backward: in gb.Z, or with `ckpt` in 8 bits there."""
     stream = _stream(stream)
     w, slot, seg_off, buf_expert, send = _route_and_dispatch(desc, x, home, e2n, b, eps, stream)
-    H, out, ffn_ws = _ptr(b.H), _ptr(b.out), _ptr(b.ffn_ws)
-    locmoe_expert_ffn_in_save_ws(desc, send, seg_off, buf_expert, W_in, H, gb.Z, ffn_ws, LOCMOE_FFN_WS_BYTES, stream)
-    locmoe_expert_ffn_out_ws(desc, H, seg_off, buf_expert, W_out, out, ffn_ws, LOCMOE_FFN_WS_BYTES, stream)
+    out = _experts_train(desc, send, seg_off, buf_expert, W_in, W_out, b, gb, ckpt, stream)
     locmoe_combine(desc, out, slot, w, b.y, stream)
     return b.y
 
 
-def backward(desc, dy, home, e2n, W_in_t, W_out_t, b: Buffers, gb: GradBuffers, eps=None, stream=None):
+def backward(desc, dy, home, e2n, W_in_t, W_out_t, b: Buffers, gb: GradBuffers, eps=None, stream=None, ckpt=None):
     """Enqueues the backward steps on one stream, in reverse order of the forward; W_in_t / W_out_t are the
-    transposed weights in the layout desc.w_packed names.  Leaves dx, dW_in, dW_out in gb."""
+    transposed weights in the layout desc.w_packed names; `ckpt` as in the forward.  Leaves dx, dW_in, dW_out in gb."""
     stream = _stream(stream)
-    slot, seg_off, buf_expert, dout, dw, dZ, dsend, dg = (_ptr(t) for t in (b.slot, b.seg_off, b.buf_expert, gb.dout, gb.dw,
-                                                                            gb.dZ, gb.dsend, gb.dg))
+    slot, seg_off, buf_expert, dout, dw, dg = (_ptr(t) for t in (b.slot, b.seg_off, b.buf_expert, gb.dout, gb.dw, gb.dg))
     locmoe_combine_bwd(desc, dy, b.out, slot, b.w, dout, dw, stream)
-    locmoe_expert_ffn_dgrad_ws(desc, dout, gb.Z, seg_off, buf_expert, W_out_t, W_in_t, dZ, dsend, b.ffn_ws,
-                               LOCMOE_FFN_WS_BYTES, stream)
-    locmoe_expert_ffn_wgrad(desc, b.send, b.H, dout, dZ, seg_off, buf_expert, gb.dW_in, gb.dW_out, stream)
+    dsend = _experts_backward(desc, dout, seg_off, buf_expert, W_in_t, W_out_t, b, gb, ckpt, stream)
     locmoe_route_bwd(desc, b.g, eps, home, e2n, b.eid, b.cnt, b.Psum, dw, gb.coef, dg, stream)
     locmoe_dispatch_bwd(desc, dsend, slot, dg, gb.dx, stream)
+    return gb.dx
+
+
+# ---- the layer in a transformer block: y = x + scale w gamma_out n(experts(n(x) gamma_in)) --------------------
+@dataclass
+class Block:
+    """The block's parameters around the layer.  gamma_in, gamma_out: device [d] fp32 or None (ones); post_norm False: no
+    norm behind the layer (gamma_out is then a scale for each channel)."""
+    gamma_in: object = None
+    gamma_out: object = None
+    post_norm: bool = True
+    norm_eps: float = 1e-5
+    scale: float = 1.0
+
+
+@dataclass
+class BlockBuffers:
+    xn: object
+    rstd_in: object
+    rstd_out: object
+    dgamma_in: object
+    dgamma_out: object
+    ws: object
+    ws_bytes: int
+    few_out: object = None     # up to LOCMOE_FEW_MAX_TOKENS tokens: the experts' outputs, a row per token, and scratch
+    few_ws: object = None
+    few_ws_bytes: int = 0
+
+
+def alloc_block_buffers(desc: locmoe_desc, device="cuda") -> BlockBuffers:
+    import torch
+    T, d = desc.T, desc.d
+    xd = torch.bfloat16 if desc.x_dtype == LOCMOE_BF16 else torch.float32
+    f32 = dict(dtype=torch.float32, device=device)
+    wsb, fewb = locmoe_norm_workspace_bytes(desc), locmoe_layer_few_workspace_bytes(desc)
+    return BlockBuffers(
+        xn=torch.empty(T, d, dtype=xd, device=device), rstd_in=torch.empty(T, **f32), rstd_out=torch.empty(T, **f32),
+        dgamma_in=torch.empty(d, **f32), dgamma_out=torch.empty(d, **f32),
+        ws=torch.empty(wsb, dtype=torch.uint8, device=device), ws_bytes=wsb,
+        few_out=torch.empty(T, d, dtype=xd, device=device) if fewb else None,
+        few_ws=torch.empty(fewb, dtype=torch.uint8, device=device) if fewb else None, few_ws_bytes=fewb)
+
+
+def _norm_and_dispatch(desc, x, home, e2n, block, b, kb, eps, stream):
+    xn, g, eid, w, slot, seg_off, buf_expert, send = (_ptr(t) for t in (kb.xn, b.g, b.eid, b.w, b.slot, b.seg_off,
+                                                                        b.buf_expert, b.send))
+    locmoe_norm_gate(desc, x, block.gamma_in, block.norm_eps, xn, kb.rstd_in, g, stream)
+    locmoe_route(desc, g, eps, home, e2n, eid, w, b.cnt, b.Psum, b.stats, b.ws, b.ws_bytes, stream)
+    locmoe_dispatch(desc, xn, eid, e2n, b.pos, slot, b.kept, seg_off, b.node_off, buf_expert, b.row_token, send, b.ws,
+                    b.ws_bytes, stream)
+    return w, slot, seg_off, buf_expert, send
+
+
+def forward_block(desc, x, home, e2n, W_in, W_out, block: Block, b: Buffers, kb: BlockBuffers, eps=None, stream=None):
+    """The block's forward: as forward, with the norms and the residual.  Leaves y in b.y."""
+    stream = _stream(stream)
+    w, slot, seg_off, buf_expert, send = _norm_and_dispatch(desc, x, home, e2n, block, b, kb, eps, stream)
+    out = _ptr(b.out)
+    locmoe_expert_ffn_ws(desc, send, seg_off, buf_expert, W_in, W_out, b.H, out, b.ffn_ws, LOCMOE_FFN_WS_BYTES, stream)
+    locmoe_combine_norm(desc, out, slot, w, x, block.gamma_out, block.post_norm, block.norm_eps, block.scale, b.y,
+                        kb.rstd_out, stream)
+    return b.y
+
+
+def decode_block(desc, x, W_in, W_out, block: Block, b: Buffers, kb: BlockBuffers, eps=None, stream=None):
+    """The block's forward for up to LOCMOE_FEW_MAX_TOKENS tokens in four launches, without statistics and send buffer:
+    leaves y in b.y, the routing in b.eid, b.w and b.slot (row m of kb.few_out for a kept token m)."""
+    stream = _stream(stream)
+    xn, g, slot, w, out = _ptr(kb.xn), _ptr(b.g), _ptr(b.slot), _ptr(b.w), _ptr(kb.few_out)
+    locmoe_norm_gate(desc, x, block.gamma_in, block.norm_eps, xn, kb.rstd_in, g, stream)
+    locmoe_layer_few(desc, xn, g, eps, W_in, W_out, False, b.eid, w, slot, out, kb.few_ws, kb.few_ws_bytes, stream)
+    locmoe_combine_norm(desc, out, slot, w, x, block.gamma_out, block.post_norm, block.norm_eps, block.scale, b.y,
+                        kb.rstd_out, stream)
+    return b.y
+
+
+def forward_block_train(desc, x, home, e2n, W_in, W_out, block: Block, b: Buffers, kb: BlockBuffers, gb: GradBuffers,
+                        eps=None, stream=None, ckpt=None):
+    """forward_block with the pre-activation kept for the backward: in gb.Z, or with `ckpt` in 8 bits there."""
+    stream = _stream(stream)
+    w, slot, seg_off, buf_expert, send = _norm_and_dispatch(desc, x, home, e2n, block, b, kb, eps, stream)
+    out = _experts_train(desc, send, seg_off, buf_expert, W_in, W_out, b, gb, ckpt, stream)
+    locmoe_combine_norm(desc, out, slot, w, x, block.gamma_out, block.post_norm, block.norm_eps, block.scale, b.y,
+                        kb.rstd_out, stream)
+    return b.y
+
+
+def backward_block(desc, dy, x, home, e2n, W_in_t, W_out_t, block: Block, b: Buffers, kb: BlockBuffers, gb: GradBuffers,
+                   eps=None, stream=None, ckpt=None):
+    """The block's backward; x as the forward had it.  Leaves dx, dW_in, dW_out in gb and dgamma_in, dgamma_out in kb."""
+    stream = _stream(stream)
+    slot, seg_off, buf_expert, dout, dw, dg = (_ptr(t) for t in (b.slot, b.seg_off, b.buf_expert, gb.dout, gb.dw, gb.dg))
+    locmoe_combine_norm_bwd(desc, dy, b.out, slot, b.w, block.gamma_out, block.post_norm, block.scale, kb.rstd_out, dout, dw,
+                            kb.dgamma_out, kb.ws, kb.ws_bytes, stream)
+    dsend = _experts_backward(desc, dout, seg_off, buf_expert, W_in_t, W_out_t, b, gb, ckpt, stream)
+    locmoe_route_bwd(desc, b.g, eps, home, e2n, b.eid, b.cnt, b.Psum, dw, gb.coef, dg, stream)
+    locmoe_dispatch_norm_bwd(desc, dsend, slot, dg, x, block.gamma_in, kb.rstd_in, dy, gb.dx, kb.dgamma_in, kb.ws,
+                             kb.ws_bytes, stream)
     return gb.dx

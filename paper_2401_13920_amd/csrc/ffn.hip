@@ -323,14 +323,40 @@ __device__ __forceinline__ void dma_tile(const DmaTile& cur, const DmaTile& nxt,
   // scratch memory (13 us per tile, with one wave per SIMD to hide it).
   int l16e = l16, kqe = kq;
   asm volatile("" : "+v"(l16e), "+v"(kqe));
+  const int nb = cur.n_base + wn * 128 + kqe * 4;  // a lane holds rows 4*(l/16)..+3 of the 16x16 tile D[n][m]
+  if constexpr (kept8(EPI)) {
+    // Two rows at a time, in a loop that moves the accumulators down.  All rows one after another are 34 KiB of code for eight
+    // (46 KiB for the backward), which a tile runs through once, and more than the instruction cache holds beside the K loop
+    // where the waves of a tile differ in their rows: T = 32 768, d = 2048, h = 8192, E = 32, 17 563 kept rows, first GEMM
+    // with the activations kept in 8 bits 763 -> 632 us (in bf16 662), d = 2560, h = 10 240, 6 312 rows 565 -> 464.
+    auto rows = [&](auto n, int j0) {
+      store_rows8<EPI, decltype(n)::value, 8, 16>(Cout, aux, cur.crow0, cur.rows_left, ldc, nb,
+                                                  [&](int j) { return (2 * (j0 + j) + wm) * 16 + l16e; },
+                                                  [&](int j, int ni) { return acc[ni][j]; });
+    };
+    if constexpr (NJ <= 3) {
+      rows(std::integral_constant<int, NJ>{}, 0);
+    } else {
+      int j0 = 0;
+#pragma nounroll
+      for (; j0 + 1 < NJ; j0 += 2) {
+        rows(std::integral_constant<int, 2>{}, j0);
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    const int m = (2 * j + wm) * 16 + l16e;
-    if (m < cur.rows_left) {
+        for (int ni = 0; ni < 8; ++ni)
 #pragma unroll
-      for (int ni = 0; ni < 8; ++ni) {
-        const int n = cur.n_base + wn * 128 + ni * 16 + kqe * 4;  // a lane holds rows 4*(l/16)..+3 of the 16x16 tile D[n][m]
-        store_quad<EPI, false>(Cout, aux, cur.crow0 + m, ldc, n, acc[ni][j][0], acc[ni][j][1], acc[ni][j][2], acc[ni][j][3]);
+          for (int j = 0; j + 2 < NJ; ++j) acc[ni][j] = acc[ni][j + 2];
+      }
+      if constexpr (NJ & 1) rows(std::integral_constant<int, 1>{}, j0);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int m = (2 * j + wm) * 16 + l16e;
+      if (m < cur.rows_left) {
+#pragma unroll
+        for (int ni = 0; ni < 8; ++ni)
+          store_quad<EPI, false>(Cout, aux, cur.crow0 + m, ldc, nb + ni * 16, acc[ni][j][0], acc[ni][j][1], acc[ni][j][2],
+                                 acc[ni][j][3]);
       }
     }
   }
@@ -586,14 +612,20 @@ __global__ __launch_bounds__(64, 1) void ffn_gemm_few(const uint16_t* __restrict
     }
 #pragma unroll
     for (int u = 0; u < D; ++u) mul(u);
+    const int nb = cg * kFewCols + kq * 4;
+    if constexpr (kept8(EPI)) {
+      store_rows8<EPI, NJ, 4, 16>(Cout, aux, (size_t)seg0 + m0, rows - m0, Ndim, nb, [&](int j) { return 16 * j + l16; },
+                                  [&](int j, int ni) { return acc[ni][j]; });
+    } else {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const int m = m0 + 16 * j + l16;
-      if (m < rows) {
+      for (int j = 0; j < NJ; ++j) {
+        const int m = m0 + 16 * j + l16;
+        if (m < rows) {
 #pragma unroll
-        for (int ni = 0; ni < 4; ++ni)
-          store_quad<EPI, false>(Cout, aux, (size_t)seg0 + m, Ndim, cg * kFewCols + 16 * ni + kq * 4, acc[ni][j][0],
-                                 acc[ni][j][1], acc[ni][j][2], acc[ni][j][3]);
+          for (int ni = 0; ni < 4; ++ni)
+            store_quad<EPI, false>(Cout, aux, (size_t)seg0 + m, Ndim, nb + 16 * ni, acc[ni][j][0], acc[ni][j][1], acc[ni][j][2],
+                                   acc[ni][j][3]);
+        }
       }
     }
   }

@@ -206,16 +206,21 @@ __device__ __forceinline__ void any_tile(const char* __restrict__ A, const char*
     fill = stage;
     stage = stage + 1 == S::kStages ? 0 : stage + 1;
   }
+  if constexpr (kept8(EPI)) {
+    store_rows8<EPI, NJ, NI, 32>((uint16_t*)Cout, aux, crow0, rows_left, Ndim, n0 + wn * 16 + kq * 4,
+                                 [&](int j) { return (2 * j + wm) * 16 + l16; }, [&](int j, int ni) { return acc[ni][j]; });
+  } else {
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    const int m = (2 * j + wm) * 16 + l16;
-    if (m < rows_left) {
+    for (int j = 0; j < NJ; ++j) {
+      const int m = (2 * j + wm) * 16 + l16;
+      if (m < rows_left) {
 #pragma unroll
-      for (int ni = 0; ni < NI; ++ni) {
-        const int n = n0 + (2 * ni + wn) * 16 + kq * 4;  // a lane holds D[n .. n+3][m]
-        if (EPI == kEpiGeluSave8 || n < Ndim)  // Ndim % 8 == 0 and n % 4 == 0: the quad is entirely inside or outside
-          store_quad<EPI, OUT_F32>(Cout, aux, crow0 + m, Ndim, n, acc[ni][j][0], acc[ni][j][1], acc[ni][j][2],
-                                   acc[ni][j][3], n < Ndim);
+        for (int ni = 0; ni < NI; ++ni) {
+          const int n = n0 + (2 * ni + wn) * 16 + kq * 4;  // a lane holds D[n .. n+3][m]
+          if (n < Ndim)  // Ndim % 8 == 0 and n % 4 == 0: the quad is entirely inside or outside
+            store_quad<EPI, OUT_F32>(Cout, aux, crow0 + m, Ndim, n, acc[ni][j][0], acc[ni][j][1], acc[ni][j][2],
+                                     acc[ni][j][3]);
+        }
       }
     }
   }

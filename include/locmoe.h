@@ -403,8 +403,10 @@ int locmoe_dispatch_norm_bwd(const locmoe_desc* desc, const void* dsend, const i
  *   here as locmoe_gate does, up to the order of the additions); eps device [E] fp32 or NULL; W_in, W_out row-major or packed
  *   as desc->w_packed says; eid, slot device [T] i32, w device [T] fp32, y device [T,d] of x_dtype (may be x itself);
  *   ws device scratch of >= locmoe_layer_few_workspace_bytes (0: an invalid descriptor, or too many tokens), nothing in it
- *   has to be set.  desc->N, alpha and mu are not used.  LOCMOE_ERR_SHAPE if T > LOCMOE_FEW_MAX_TOKENS. */
+ *   has to be set.  desc->N, alpha and mu are not used.  LOCMOE_ERR_SHAPE if T > LOCMOE_FEW_MAX_TOKENS
+ *   or d or h > LOCMOE_FEW_MAX_WIDTH. */
 #define LOCMOE_FEW_MAX_TOKENS 64
+#define LOCMOE_FEW_MAX_WIDTH (1 << 26)
 size_t locmoe_layer_few_workspace_bytes(const locmoe_desc* desc);
 int locmoe_layer_few(const locmoe_desc* desc, const void* x, const float* g, const float* eps, const void* W_in,
                      const void* W_out, int32_t weighted, int32_t* eid, float* w, int32_t* slot, void* y, void* ws,

@@ -114,6 +114,17 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
+// The same for an L known at run time (the same in all lanes)
+__device__ __forceinline__ float lanes_sum(float v, int L) {
+  if (L >= 2) v += dpp_f32<kDppXor1>(v);
+  if (L >= 4) v += dpp_f32<kDppXor2>(v);
+  if (L >= 8) v += dpp_f32<kDppHalfMirror>(v);
+  if (L >= 16) v += dpp_f32<kDppMirror>(v);
+  if (L >= 32) v += __shfl_xor(v, 16);
+  if (L >= 64) v += __shfl_xor(v, 32);
+  return v;
+}
+
 // ---- direct global -> LDS copies -------------------------------------------------------------
 typedef const char __attribute__((address_space(3))) * lds_cptr;
 

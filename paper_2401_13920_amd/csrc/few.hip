@@ -18,6 +18,7 @@
 
 #include "common.h"
 #include "ffn_epilogue.h"
+#include "gelu_coef_f32.h"
 
 namespace locmoe {
 namespace {
@@ -26,6 +27,10 @@ constexpr int kFewTokens = LOCMOE_FEW_MAX_TOKENS;
 static_assert(kFewTokens == kWave, "the routing of all tokens is one wave's");
 constexpr int kFewThreads = 512, kFewWaves = kFewThreads / kWave;
 constexpr int kFewRowsTile = 16;
+// Packed weights of more than this in one launch, which the last-level cache does not hold until the next call anyway, are loaded
+// past it: d = 4096, h = 16384, 24 experts 1 105 -> 1 024 us; d = 1024, h = 4096, one expert 12.9 -> 14.6.  Not row-major ones,
+// of whose lines a load takes half: the other half is fetched again.
+constexpr long long kFewStreamBytes = 100ll << 20;
 
 // The routing as the second kernel reads it (front of the workspace; H follows at kFewHOffset)
 struct FewTable {
@@ -37,91 +42,123 @@ struct FewTable {
 constexpr size_t kFewHOffset = 1024;
 static_assert(sizeof(FewTable) <= kFewHOffset, "");
 
-// fp32 -> three bf16 parts whose sum is the value (cut, so that every remainder is exact).  An infinity or a NaN is the first
-// part alone.
-__device__ __forceinline__ void split3(float v, uint32_t (&p)[3]) {
-  uint32_t b = __float_as_uint(v);
-  p[0] = b >> 16;
-  const bool fin = fabsf(v) < INFINITY;
-  if ((b & 0x7F800000u) == 0x7F800000u) p[0] |= (b & 0xFFFFu) ? 1u : 0u;  // (a NaN stays one)
-  float r = fin ? v - __uint_as_float(b & 0xFFFF0000u) : 0.f;
-  b = __float_as_uint(r);
-  p[1] = b >> 16;
-  r -= __uint_as_float(b & 0xFFFF0000u);
-  p[2] = __float_as_uint(r) >> 16;
+// Two fp32 values -> three bf16 parts of each (bits 0..7, 8..15 and 16..23 of the significand: cut, so that every remainder is
+// exact), the first value's in the low halves.  An infinity leaves NaN for its second part.
+__device__ __forceinline__ void split3(float a, float b, uint32_t (&p)[3]) {
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
+    p[k] = __builtin_amdgcn_perm(ub, ua, 0x07060302u);  // the upper halves
+    a -= __uint_as_float(ua & 0xFFFF0000u);
+    b -= __uint_as_float(ub & 0xFFFF0000u);
+  }
 }
 
-// GeLU of a value that is kept in fp32
-__device__ __forceinline__ float gelu_f32(float z) { return z * (0.5f * erfcf(-0.70710678118654752f * z)); }
+// GeLU of a value that is kept in fp32: as gelu_bf16, with a polynomial whose error is below 8e-8 |v|
+__device__ __forceinline__ float gelu_f32(float v) {
+  const float x = __builtin_amdgcn_fmed3f(fabsf(v), 0.f, kGeluXMax);
+  float q = kGeluCoefF32[kGeluDegreeF32];
+#pragma unroll
+  for (int k = kGeluDegreeF32 - 1; k >= 0; --k) q = fmaf(q, x, kGeluCoefF32[k]);
+  return 0.5f * fmaf(-x, __builtin_amdgcn_exp2f(q), v + fabsf(v));
+}
 
-// Gating value of token m for expert e by L lanes (this one the l-th): its share of the block's sum
+// Eight loads in flight of a lane's share of the sum over the blk features from x[at] on: every L-th 16-byte chunk (or feature,
+// where chunks do not fit) from the l-th on; L = 2^lL
 template <bool BF16>
-__device__ __forceinline__ float gate_part(const void* x, int m, int e, int d, int blk, int l, int L) {
-  constexpr int V = BF16 ? 8 : 4;
+__device__ __forceinline__ float gate_part(const void* x, size_t at, int blk, int l, int lL) {
+  constexpr int V = BF16 ? 8 : 4, U = 8;
   float s = 0.f;
-  const size_t at = (size_t)m * d + (size_t)e * blk;
   if (blk % V == 0) {  // (rows are whole chunks too)
     const uint4* p = (const uint4*)x + at / V;
-    for (int c = l; c < blk / V; c += L) s += BF16 ? sum8_bf16(p[c]) : sum4_f32(p[c]);
+    const int n = blk / V;
+    for (int c = l; c < n; c += U << lL) {
+      uint4 v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = p[min(c + (u << lL), n - 1)];
+#pragma unroll
+      for (int u = 0; u < U; ++u) s += c + (u << lL) < n ? (BF16 ? sum8_bf16(v[u]) : sum4_f32(v[u])) : 0.f;
+    }
   } else {
-    for (int c = l; c < blk; c += L) s += BF16 ? bf16_bits_to_f32(((const uint16_t*)x)[at + c]) : ((const float*)x)[at + c];
+    for (int c = l; c < blk; c += 1 << lL) s += BF16 ? bf16_bits_to_f32(((const uint16_t*)x)[at + c]) : ((const float*)x)[at + c];
   }
   return s;
 }
 
-// Top-1 of token m by one wave: eid and score to LDS.  Experts are lane e (L lanes each while E < 64), e + 64, ...
+// How a work-group routes all tokens: S lanes share a token, as many as let every token have its own, so that all of them wait for
+// their loads together; P experts side by side (the next ones in further turns), S / P lanes each.  Powers of two.
+struct FewRoute {
+  int lS, lP, blk;
+  float inv_blk;
+};
+FewRoute few_route_plan(int T, int d, int E) {
+  FewRoute r = {6, 0, d / E, 1.0f / (float)(d / E)};
+  while ((T << r.lS) > kFewThreads) --r.lS;
+  while (r.lP < r.lS && (1 << r.lP) < E) ++r.lP;
+  return r;
+}
+
+// Top-1 of all tokens by the work-group: eid and score to LDS.  The largest value and the sum of exponentials up to it are kept
+// as the experts go by.  Short rather than unrolled: a launch of this size spends much of its time fetching and issuing its own
+// instructions (16 tokens, d = 128, E = 8, fp32, this kernel: 13.6 us with the experts' turns unrolled and a long GeLU, 7.3 so).
 template <bool BF16>
-__device__ __forceinline__ void few_route(const void* x, const float* g, const float* eps, int m, int d, int E, int relu,
-                                          int32_t* s_eid, float* s_w) {
-  const int lane = threadIdx.x & 63, blk = d / E;
-  int L = 1;
-  while (2 * L * E <= kWave) L *= 2;
-  float best = -INFINITY;
-  int at = 0x7FFFFFFF;
-  const float inv = 1.0f / (float)blk;
-  float val[16];  // E <= 1024
-#pragma unroll
-  for (int k = 0; k < 16; ++k) {
-    const int e = lane / L + k * kWave;
-    val[k] = -INFINITY;
-    if (k * kWave >= E) continue;
-    float v = 0.f;
-    if (e < E) v = g ? g[(size_t)m * E + e] : gate_part<BF16>(x, m, e, d, blk, lane % L, L);
-    if (!g) {
-      for (int o = 1; o < L; o *= 2) v += __shfl_xor(v, o);
-      v *= inv;
-    }
-    if (e < E) {
+__device__ __forceinline__ void few_route(const FewRoute& r, const void* x, const float* g, const float* eps, int T, int d, int E,
+                                          int relu, int32_t* s_eid, float* s_w) {
+  const int S = 1 << r.lS, P = 1 << r.lP, lL = r.lS - r.lP, L = 1 << lL, l = threadIdx.x & (S - 1);
+  constexpr float kLog2e = 1.44269504f;
+  {  // (S T <= kFewThreads: every token has its lanes; the lanes left over repeat the last one)
+    const int m0 = threadIdx.x >> r.lS, m = min(m0, T - 1);
+    float best = -INFINITY, z = 0.f;
+    int at = E;
+    auto seen = [&](int e, float v) {
       if (eps) v += eps[e];
       if (relu) v = fmaxf(v, 0.f);
-      val[k] = v;
-      if (v > best || at == 0x7FFFFFFF) { best = v; at = e; }  // (ascending e: ties stay with the lower)
+      const float f = __builtin_amdgcn_exp2f(-kLog2e * fabsf(v - best));
+      const bool more = v > best || at == E;  // (ascending e: ties stay with the lower)
+      z = more ? fmaf(z, f, 1.0f) : z + f;
+      best = more ? v : best;
+      at = more ? e : at;
+    };
+    if (g) {
+#pragma unroll 4
+      for (int e = l >> lL; e < E; e += P) seen(e, g[(size_t)m * E + e]);
+    } else {
+      for (int e = l >> lL; e < E; e += P)
+        seen(e, lanes_sum(gate_part<BF16>(x, (size_t)m * d + (size_t)e * r.blk, r.blk, l & (L - 1), lL), L) * r.inv_blk);
     }
+    float top = best;
+    int who = at;
+    for (int o = S / 2; o > 0; o >>= 1) {
+      const float ov = __shfl_xor(top, o);
+      const int oa = __shfl_xor(who, o);
+      const bool take = who == E || (oa < E && (ov > top || (ov == top && oa < who)));
+      top = take ? ov : top;
+      who = take ? oa : who;
+    }
+    const float sum = lanes_sum(at < E && (l & (L - 1)) == 0 ? z * __builtin_amdgcn_exp2f(kLog2e * (best - top)) : 0.f, S);
+    if (l == 0 && m0 < T) { s_eid[m] = who; s_w[m] = 1.0f / sum; }
   }
-  for (int o = 32; o > 0; o >>= 1) {
-    const float ov = __shfl_xor(best, o);
-    const int oa = __shfl_xor(at, o);
-    if (oa != 0x7FFFFFFF && (at == 0x7FFFFFFF || ov > best || (ov == best && oa < at))) { best = ov; at = oa; }
-  }
-  float z = 0.f;
-#pragma unroll
-  for (int k = 0; k < 16; ++k)
-    if (k * kWave < E && lane / L + k * kWave < E && lane % L == 0) z += expf(val[k] - best);
-  z = group_sum<kWave>(z);
-  if (lane == 0) { s_eid[m] = at; s_w[m] = 1.0f / z; }
 }
 
 // The groups, by one wave (lane m: token m): first-come capacity, groups in the order of their first tokens
 __device__ __forceinline__ void few_groups(const int32_t* s_eid, int T, int C, FewTable* t, int32_t* s_slot) {
   const int m = threadIdx.x;
-  const int e = m < T ? s_eid[m] : -1;
-  int pos = 0, all = 0;
-  for (int q = 0; q < T; ++q) {
-    const bool same = s_eid[q] == e;
-    pos += same && q < m;
-    all += same;
+  if (T == 1) {  // (a single sequence's decoding)
+    if (m == 0) { t->groups = 1; t->expert[0] = s_eid[0]; t->start[0] = 0; t->start[1] = 1; t->token[0] = 0; s_slot[0] = 0; }
+    return;
   }
-  const bool live = m < T, first = live && pos == 0;
+  const bool live = m < T;
+  const int e = live ? s_eid[m] : 0;
+  uint64_t same = __ballot(live);  // the tokens of the same expert: a vote on every bit of its number (E <= 1024)
+#pragma unroll
+  for (int b = 0; b < 10; ++b) {
+    const uint64_t ones = __ballot((e >> b) & 1);
+    same &= (e >> b) & 1 ? ones : ~ones;
+  }
+  const uint64_t below = (1ull << m) - 1ull;
+  const int pos = __builtin_popcountll(same & below), all = __builtin_popcountll(same);
+  const int lead = live ? __builtin_ctzll(same) : 0;  // the lane that leads this token's group
+  const bool first = live && pos == 0;
   const uint64_t leaders = __ballot(first);
   const int n = first ? min(all, C) : 0;  // kept tokens of the group that this lane leads
   int sum = n;                            // inclusive over the leaders up to this lane
@@ -129,12 +166,8 @@ __device__ __forceinline__ void few_groups(const int32_t* s_eid, int T, int C, F
     const int up = __shfl_up(sum, o);
     if (m >= o) sum += up;
   }
-  int lead = 0;  // the lane that leads this token's group
-  for (int q = T - 1; q >= 0; --q)
-    if (s_eid[q] == e) lead = q;
-  const int start = __shfl(sum - n, lead);
+  const int start = __shfl(sum - n, lead), u = __builtin_popcountll(leaders & below);
   if (first) {
-    const int u = __builtin_popcountll(leaders & ((1ull << m) - 1ull));
     t->expert[u] = e;
     t->start[u] = sum - n;
   }
@@ -147,130 +180,161 @@ __device__ __forceinline__ void few_groups(const int32_t* s_eid, int T, int C, F
   }
 }
 
-// A group's share of a GEMM: the KS-th part of K of one 16-row tile of weights by one wave, NB column tiles of 16 tokens.
-// W: the expert's weights.  Operand B is the tokens' rows: bf16 (X_F32 false, NP planes `plane` elements apart) or fp32.
-template <bool PACKED, bool X_F32, int NP, int NB>
+// k-steps in flight: what 128 registers hold beside the sums (x 16-byte loads of the tokens' operand a step).  16 waves of a compute
+// unit have 128 KiB of weights in flight with 8.  (Pairs of tiles, which fetch the tokens' operand half as often, are slower: 20
+// experts of d = 1024, h = 4096 83 -> 107 us, d = 4096, h = 16384 902 -> 931; so are loads kept in flight across the products,
+// 1 025 -> 1 058.)
+constexpr int few_depth(int x) { return x <= 1 ? 8 : x <= 3 ? 4 : x <= 6 ? 2 : 1; }
+
+// A wave's share of a GEMM: steps s0 .. s1 - 1 of K for one 16-row tile of weights and NB column tiles of 16 tokens.  W: the
+// expert's weights.  Operand B is the tokens' rows: bf16 (NP planes `plane` elements apart) or, with X_F32, fp32.  STREAM: the
+// weights are loaded past the caches.
+template <bool PACKED, bool X_F32, int NP, int NB, bool STREAM>
 __device__ __forceinline__ void few_dot(f32x4 (&acc)[NB], const char* __restrict__ W, const void* __restrict__ X,
                                         size_t plane, const int32_t* tok, int n, int tile, int Kdim, int Ndim, int s0,
                                         int s1) {
-  constexpr int D = NB * NP <= 2 ? 8 : NB * NP <= 4 ? 4 : 2;  // k-steps whose weights are in flight
+  constexpr int XL = X_F32 ? 2 : NP;  // 16-byte loads of a column tile and step
+  constexpr int D = few_depth(NB * XL);
   const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
-  const int row = min(tile * kFewRowsTile + l16, Ndim - 1);
-  const char* pw;
-  size_t wstep;
-  if (PACKED) {
-    pw = W + (size_t)(row >> 8) * Kdim * 512 + (row & 255) * 64 + ((q ^ ((row >> 1) & 3)) << 4);
-    wstep = 16384;
-  } else {
-    pw = W + (size_t)row * Kdim * 2 + q * 16;
-    wstep = 64;
-  }
+  constexpr int kStep = PACKED ? 16384 : 64, kXStep = X_F32 ? 128 : 64;
+  const int row = min(tile * kFewRowsTile + l16, Ndim - 1);  // (rows past the last repeat it: not stored)
+  const char* pw = PACKED ? W + (size_t)(row >> 8) * Kdim * 512 + (row & 255) * 64 + ((q ^ ((row >> 1) & 3)) << 4)
+                          : W + (size_t)row * Kdim * 2 + q * 16;
   const char* px[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b)  // columns past the group's tokens repeat the last one (not stored)
     px[b] = (const char*)X + ((size_t)tok[min(16 * b + l16, n - 1)] * Kdim + q * 8) * (X_F32 ? 4 : 2);
 #pragma unroll
   for (int b = 0; b < NB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  // steps s .. s + D - 1; TAIL: the one step that ends behind K, where both operands are zeros past it
-  auto steps = [&](auto depth, auto tail, int s) {
-    constexpr int D = decltype(depth)::value;
-    constexpr bool TAIL = decltype(tail)::value;
-    u32x4 w[D], x[D][NB][X_F32 ? 2 : NP];
-    const u32x4 zero = {0u, 0u, 0u, 0u};
-    const bool in = !TAIL || s * 32 + q * 8 < Kdim;
+  u32x4 w[D], x[D][NB][XL];
+  auto load = [&](int u, int s) {
+    const u32x4* p = (const u32x4*)(pw + (size_t)s * kStep);
+    w[u] = STREAM ? __builtin_nontemporal_load(p) : *p;
 #pragma unroll
-    for (int u = 0; u < D; ++u) {
-      w[u] = in ? *(const u32x4*)(pw + (size_t)(s + u) * wstep) : zero;
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int p = 0; p < (X_F32 ? 2 : NP); ++p) {
-          const char* a = px[b] + (X_F32 ? (size_t)(s + u) * 128 + p * 16 : (size_t)(s + u) * 64 + p * plane * 2);
-          x[u][b][p] = in ? *(const u32x4*)a : zero;
-        }
-    }
-#pragma unroll
-    for (int u = 0; u < D; ++u)
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        u32x4 part[NP];
-        if constexpr (X_F32) {
-          uint32_t v[8][3];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) split3(__uint_as_float(x[u][b][i / 4][i % 4]), v[i]);
-#pragma unroll
-          for (int p = 0; p < NP; ++p)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) part[p][i] = v[2 * i][p] | (v[2 * i + 1][p] << 16);
-        } else {
-#pragma unroll
-          for (int p = 0; p < NP; ++p) part[p] = x[u][b][p];
-        }
-#pragma unroll
-        for (int p = 0; p < NP; ++p)
-          acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[u]),
-                                                           __builtin_bit_cast(bf16x8, part[p]), acc[b], 0, 0, 0);
-      }
+      for (int p = 0; p < XL; ++p)
+        x[u][b][p] = *(const u32x4*)(px[b] + (size_t)s * kXStep + (X_F32 ? p * 16 : p * plane * 2));
   };
-  using No = std::false_type;
-  const int full = min(s1, Kdim / 32);
-  int s = s0;
-  for (; s + D <= full; s += D) steps(std::integral_constant<int, D>{}, No{}, s);
-  if constexpr (D > 4) { if (s + 4 <= full) { steps(std::integral_constant<int, 4>{}, No{}, s); s += 4; } }
-  if constexpr (D > 2) { if (s + 2 <= full) { steps(std::integral_constant<int, 2>{}, No{}, s); s += 2; } }
-  if constexpr (D > 1) { if (s < full) { steps(std::integral_constant<int, 1>{}, No{}, s); ++s; } }
-  if (s < s1) steps(std::integral_constant<int, 1>{}, std::true_type{}, s);
+  auto mul = [&](int u) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      u32x4 part[NP];
+      if constexpr (X_F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t v[3];
+          split3(__uint_as_float(x[u][b][i / 2][2 * i % 4]), __uint_as_float(x[u][b][i / 2][2 * i % 4 + 1]), v);
+#pragma unroll
+          for (int p = 0; p < NP; ++p) part[p][i] = v[p];
+        }
+      } else {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) part[p] = x[u][b][p];
+      }
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+        acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[u]), __builtin_bit_cast(bf16x8, part[p]),
+                                                         acc[b], 0, 0, 0);
+    }
+  };
+  // Whole turns of D steps, in a cycle that begins at a place of its own in each of 16 neighbouring blocks of packed rows: in
+  // step, all waves read at multiples of a power of two, which are few of the memory's channels (d = 4096, h = 16384, 20
+  // experts: 952 -> 890 us).
+  const int full = min(s1, Kdim / 32), turns = max(full - s0, 0) / D;
+  int at = s0 + (PACKED ? (tile >> 4) & 15 : 0) * (turns >> 4) * D;
+  for (int i = 0; i < turns; ++i) {
+#pragma unroll
+    for (int u = 0; u < D; ++u) load(u, at + u);
+#pragma unroll
+    for (int u = 0; u < D; ++u) mul(u);
+    at += D;
+    if (at == s0 + turns * D) at = s0;
+  }
+  int s = s0 + turns * D;
+  // fewer than D steps are left: all their loads, then all their products
+#pragma unroll
+  for (int u = 0; u < D - 1; ++u)
+    if (s + u < full) load(u, s + u);
+#pragma unroll
+  for (int u = 0; u < D - 1; ++u)
+    if (s + u < full) mul(u);
+  s = max(s, full);
+  if (s < s1) {  // the step that ends behind K, where both operands are zeros past it
+    const u32x4 zero = {0u, 0u, 0u, 0u};
+    w[0] = zero;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int p = 0; p < XL; ++p) x[0][b][p] = zero;
+    if (s * 32 + q * 8 < Kdim) load(0, s);
+    mul(0);
+  }
 }
 
-// All tiles of all groups, over the grid's waves: epilogue(u, tile, token's place in the group, row of weights, 4 sums).
-// MAXB: column tiles at most (of all tokens).
+// All tiles of all groups, over the grid's waves: epilogue(token, first row of weights, 4 sums).  MAXB: column tiles at most (of all
+// tokens).  per_wave: 1 / waves of the grid.  red: LDS for the sums of a tile's waves but the first.
+constexpr int few_red(int maxb) { return (kFewWaves - 1) * maxb * 64; }
 template <bool PACKED, bool X_F32, int NP, int MAXB, class F>
 __device__ __forceinline__ void few_gemm(const FewTable* t, const char* W, const void* X, size_t plane, int Kdim, int Ndim,
-                                         float4* red, F&& epilogue) {
+                                         float per_wave, float4* red, F&& epilogue) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int tiles = (Ndim + kFewRowsTile - 1) / kFewRowsTile, steps = (Kdim + 31) / 32;
-  const long long items = (long long)t->groups * tiles;
-  int ks = 1;  // waves per tile
-  while (ks < kFewWaves && items * ks < (long long)gridDim.x * kFewWaves && steps >= 4 * ks) ks *= 2;
-  const int per = kFewWaves / ks, sub = wave % ks, mine = wave / ks;
-  const int s0 = (int)((long long)steps * sub / ks), s1 = (int)((long long)steps * (sub + 1) / ks);
-  for (long long i0 = (long long)blockIdx.x * per; i0 < items; i0 += (long long)gridDim.x * per) {
-    const long long item = i0 + mine;
-    const bool have = item < items;
-    const int u = have ? (int)(item / tiles) : 0, tile = have ? (int)(item % tiles) : 0;
-    const int32_t* tok = t->token + t->start[u];
-    const int n = t->start[u + 1] - t->start[u];
-    const char* We = W + (size_t)t->expert[u] * Ndim * Kdim * 2;
-    f32x4 acc[MAXB];
-#define LOCMOE_FEW_DOT(NB)                                                                                     \
-  {                                                                                                            \
-    f32x4 a[NB];                                                                                               \
-    few_dot<PACKED, X_F32, NP, NB>(a, We, X, plane, tok, n, tile, Kdim, Ndim, s0, s1);                         \
-    _Pragma("unroll") for (int b = 0; b < NB; ++b) acc[b] = a[b];                                              \
+  const unsigned tiles = (unsigned)(Ndim + kFewRowsTile - 1) / kFewRowsTile, items = t->groups * tiles;
+  const int steps = (Kdim + 31) / 32;
+  const bool stream = PACKED && (long long)t->groups * Ndim * Kdim * 2 > kFewStreamBytes;
+  // 2^lks waves per tile: the fewest k-steps one after another, counting four for a turn of tiles' latency
+  int lks = 0;
+  float least = 3e38f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float turns = ceilf((float)(items << i) * per_wave);
+    const float cost = turns * (float)(((steps - 1) >> i) + 5);
+    if (cost < least) { least = cost; lks = i; }
   }
+  const int ks = 1 << lks, per = kFewWaves >> lks, sub = wave & (ks - 1), mine = wave >> lks;
+  const int s0 = steps * sub >> lks, s1 = steps * (sub + 1) >> lks;
+  int u = 0;
+  unsigned at = blockIdx.x * per + mine;  // number in group u
+  for (unsigned i0 = blockIdx.x * per; i0 < items; i0 += gridDim.x * per, at += gridDim.x * per) {
+    const bool have = i0 + mine < items;
+    if (have)
+      while (at >= tiles) { at -= tiles; ++u; }
+    const int tile = have ? (int)at : 0;
+    const int first = __builtin_amdgcn_readfirstlane(t->start[u]);
+    const int32_t* tok = t->token + first;
+    const int n = __builtin_amdgcn_readfirstlane(t->start[u + 1]) - first;
+    const char* We = W + (size_t)__builtin_amdgcn_readfirstlane(t->expert[u]) * Ndim * Kdim * 2;
+    f32x4 acc[MAXB];
+    auto dot = [&](auto nb_) {
+      constexpr int NB = decltype(nb_)::value;
+      f32x4 part[NB];
+      if (stream) few_dot<PACKED, X_F32, NP, NB, PACKED>(part, We, X, plane, tok, n, tile, Kdim, Ndim, s0, s1);
+      else few_dot<PACKED, X_F32, NP, NB, false>(part, We, X, plane, tok, n, tile, Kdim, Ndim, s0, s1);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) acc[b] = part[b];
+    };
     if (have) {
-      if (MAXB == 1 || n <= 16) LOCMOE_FEW_DOT(1)
+      if (MAXB == 1 || n <= 16) dot(std::integral_constant<int, 1>{});
       else if constexpr (MAXB > 1) {
-        if (n <= 32) LOCMOE_FEW_DOT(2)
-        else LOCMOE_FEW_DOT(4)
+        if (n <= 32) dot(std::integral_constant<int, 2>{});
+        else dot(std::integral_constant<int, 4>{});
       }
     }
-#undef LOCMOE_FEW_DOT
     const int nb = (n + 15) / 16;
     if (ks > 1) {
-      __syncthreads();
+      float4* sums = red + mine * (ks - 1) * (MAXB * 64) + lane;
       if (have && sub) {
 #pragma unroll
         for (int b = 0; b < MAXB; ++b)
-          if (b < nb) red[(wave * MAXB + b) * 64 + lane] = make_float4(acc[b][0], acc[b][1], acc[b][2], acc[b][3]);
+          if (b < nb) sums[((sub - 1) * MAXB + b) * 64] = make_float4(acc[b][0], acc[b][1], acc[b][2], acc[b][3]);
       }
       __syncthreads();
       if (have && !sub) {
-        for (int j = 1; j < ks; ++j)
+        for (int j = 0; j < ks - 1; ++j)
 #pragma unroll
           for (int b = 0; b < MAXB; ++b)
             if (b < nb) {
-              const float4 v = red[((wave + j) * MAXB + b) * 64 + lane];
+              const float4 v = sums[(j * MAXB + b) * 64];
               acc[b][0] += v.x; acc[b][1] += v.y; acc[b][2] += v.z; acc[b][3] += v.w;
             }
       }
@@ -282,25 +346,26 @@ __device__ __forceinline__ void few_gemm(const FewTable* t, const char* W, const
         if (c < n && r < Ndim) epilogue(tok[c], r, acc[b]);  // (Ndim is a multiple of 8: the quad is inside or outside)
       }
     }
+    if (ks > 1 && i0 + gridDim.x * per < items) __syncthreads();  // (red has been read)
   }
 }
 
-// waves per SIMD: two work-groups per compute unit, or one where the tokens' operands take the registers
-constexpr int few_occupancy(int maxb) { return maxb == 1 ? 4 : 2; }
+// (four waves per SIMD: two work-groups per compute unit)
 
 template <bool BF16, bool PACKED, int MAXB>
-__global__ __launch_bounds__(kFewThreads, few_occupancy(MAXB)) void few_in_kernel(const void* __restrict__ x, const float* __restrict__ g,
+__global__ __launch_bounds__(kFewThreads, 4) void few_in_kernel(const void* __restrict__ x, const float* __restrict__ g,
                                                                 const float* __restrict__ eps,
                                                                 const char* __restrict__ W, int32_t* __restrict__ eid,
                                                                 float* __restrict__ w, int32_t* __restrict__ slot,
                                                                 FewTable* __restrict__ table, uint16_t* __restrict__ H,
-                                                                int T, int d, int E, int h, int C, int relu) {
+                                                                int T, int d, int E, int h, int C, int relu, FewRoute plan,
+                                                                float per_wave) {
   __shared__ int32_t s_eid[kFewTokens], s_slot[kFewTokens];
   __shared__ float s_w[kFewTokens];
   __shared__ FewTable t;
-  __shared__ float4 red[kFewWaves * MAXB * 64];
+  __shared__ float4 red[few_red(MAXB)];
   const int wave = threadIdx.x >> 6;
-  for (int m = wave; m < T; m += kFewWaves) few_route<BF16>(x, g, eps, m, d, E, relu, s_eid, s_w);
+  few_route<BF16>(plan, x, g, eps, T, d, E, relu, s_eid, s_w);
   __syncthreads();
   if (wave == 0) few_groups(s_eid, T, C, &t, s_slot);
   __syncthreads();
@@ -314,30 +379,29 @@ __global__ __launch_bounds__(kFewThreads, few_occupancy(MAXB)) void few_in_kerne
   }
   constexpr int NP = BF16 ? 1 : 3;
   const size_t plane = (size_t)T * h;
-  few_gemm<PACKED, !BF16, NP, MAXB>(&t, W, x, 0, d, h, red, [&](int m, int r, const f32x4& a) {
+  few_gemm<PACKED, !BF16, NP, MAXB>(&t, W, x, 0, d, h, per_wave, red, [&](int m, int r, const f32x4& a) {
     uint16_t* dst = H + (size_t)m * h + r;
     if constexpr (BF16) {
       *(uint2*)dst = make_uint2(pack_bf16x2(gelu_bf16(a[0]), gelu_bf16(a[1])), pack_bf16x2(gelu_bf16(a[2]), gelu_bf16(a[3])));
     } else {
-      uint32_t v[4][3];
+      uint32_t lo[3], hi[3];
+      split3(gelu_f32(a[0]), gelu_f32(a[1]), lo);
+      split3(gelu_f32(a[2]), gelu_f32(a[3]), hi);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) split3(gelu_f32(a[i]), v[i]);
-#pragma unroll
-      for (int p = 0; p < 3; ++p)
-        *(uint2*)(dst + p * plane) = make_uint2(v[0][p] | (v[1][p] << 16), v[2][p] | (v[3][p] << 16));
+      for (int p = 0; p < 3; ++p) *(uint2*)(dst + p * plane) = make_uint2(lo[p], hi[p]);
     }
   });
 }
 
 template <bool BF16, bool PACKED, int MAXB>
-__global__ __launch_bounds__(kFewThreads, few_occupancy(MAXB)) void few_out_kernel(const uint16_t* __restrict__ H,
+__global__ __launch_bounds__(kFewThreads, 4) void few_out_kernel(const uint16_t* __restrict__ H,
                                                                  const FewTable* __restrict__ table,
                                                                  const int32_t* __restrict__ slot,
                                                                  const float* __restrict__ w,
                                                                  const char* __restrict__ W, void* __restrict__ y, int T,
-                                                                 int d, int h, int weighted) {
+                                                                 int d, int h, int weighted, float per_wave) {
   __shared__ FewTable t;
-  __shared__ float4 red[kFewWaves * MAXB * 64];
+  __shared__ float4 red[few_red(MAXB)];
   for (int i = threadIdx.x; i < (int)(sizeof(FewTable) / 4); i += kFewThreads) ((int32_t*)&t)[i] = ((const int32_t*)table)[i];
   __syncthreads();
   if (weighted) {  // dropped tokens
@@ -346,7 +410,7 @@ __global__ __launch_bounds__(kFewThreads, few_occupancy(MAXB)) void few_out_kern
       if (slot[m] < 0)
         for (int c = threadIdx.x; c < chunks; c += kFewThreads) ((uint4*)y)[(size_t)m * chunks + c] = make_uint4(0, 0, 0, 0);
   }
-  few_gemm<PACKED, false, BF16 ? 1 : 3, MAXB>(&t, W, H, (size_t)T * h, h, d, red, [&](int m, int r, const f32x4& a) {
+  few_gemm<PACKED, false, BF16 ? 1 : 3, MAXB>(&t, W, H, (size_t)T * h, h, d, per_wave, red, [&](int m, int r, const f32x4& a) {
     const float f = weighted ? w[m] : 1.0f;
     if constexpr (BF16)
       *(uint2*)((uint16_t*)y + (size_t)m * d + r) = make_uint2(pack_bf16x2(f * a[0], f * a[1]), pack_bf16x2(f * a[2], f * a[3]));
@@ -360,7 +424,7 @@ __global__ __launch_bounds__(kFewThreads, few_occupancy(MAXB)) void few_out_kern
 
 extern "C" size_t locmoe_layer_few_workspace_bytes(const locmoe_desc* desc) {
   using namespace locmoe;
-  if (check_desc(desc) != LOCMOE_OK || desc->T > kFewTokens) return 0;
+  if (check_desc(desc) != LOCMOE_OK || desc->T > kFewTokens || std::max(desc->d, desc->h) > LOCMOE_FEW_MAX_WIDTH) return 0;
   const size_t planes = desc->x_dtype == LOCMOE_BF16 ? 1 : 3;
   return (kFewHOffset + planes * (size_t)desc->T * (size_t)desc->h * 2 + 255) & ~(size_t)255;
 }
@@ -372,7 +436,7 @@ extern "C" int locmoe_layer_few(const locmoe_desc* desc, const void* x, const fl
   if (!desc || !x || !W_in || !W_out || !eid || !w || !slot || !y) return LOCMOE_ERR_NULL;
   const int st = check_desc(desc);
   if (st != LOCMOE_OK) return st;
-  if (desc->T > kFewTokens) return LOCMOE_ERR_SHAPE;
+  if (desc->T > kFewTokens || std::max(desc->d, desc->h) > LOCMOE_FEW_MAX_WIDTH) return LOCMOE_ERR_SHAPE;
   if (weighted != 0 && weighted != 1) return LOCMOE_ERR_ARG;
   const bool bf = desc->x_dtype == LOCMOE_BF16;
   if (desc->w_packed && (!bf || locmoe_packed_weights_bytes(desc) == 0)) return LOCMOE_ERR_ARG;
@@ -382,16 +446,18 @@ extern "C" int locmoe_layer_few(const locmoe_desc* desc, const void* x, const fl
   FewTable* table = (FewTable*)ws;
   uint16_t* H = (uint16_t*)((char*)ws + kFewHOffset);
   // two work-groups per compute unit, no more than there can be tiles (of up to eight waves each)
-  auto grid = [&](int n) {
-    return dim3((unsigned)std::min<long long>(2 * cu_count(), (long long)std::min(T, E) * ceil_div(n, kFewRowsTile)));
+  auto groups = [&](int n) {
+    return (unsigned)std::min<long long>(2 * cu_count(), (long long)std::min(T, E) * ceil_div(n, kFewRowsTile));
   };
+  const FewRoute plan = few_route_plan(T, d, E);
   auto launch = [&](auto bf16, auto packed, auto maxb) {
     constexpr bool BF = decltype(bf16)::value, PK = decltype(packed)::value;
     constexpr int MAXB = decltype(maxb)::value;
-    hipLaunchKernelGGL((few_in_kernel<BF, PK, MAXB>), grid(h), dim3(kFewThreads), 0, s, x, g, eps, (const char*)W_in, eid, w,
-                       slot, table, H, T, d, E, h, desc->C, desc->relu);
-    hipLaunchKernelGGL((few_out_kernel<BF, PK, MAXB>), grid(d), dim3(kFewThreads), 0, s, H, table, slot, w,
-                       (const char*)W_out, y, T, d, h, weighted);
+    const unsigned in = groups(h), out = groups(d);
+    hipLaunchKernelGGL((few_in_kernel<BF, PK, MAXB>), dim3(in), dim3(kFewThreads), 0, s, x, g, eps, (const char*)W_in, eid, w, slot, table, H, T, d, E, h,
+                       desc->C, desc->relu, plan, 1.0f / (float)(in * kFewWaves));
+    hipLaunchKernelGGL((few_out_kernel<BF, PK, MAXB>), dim3(out), dim3(kFewThreads), 0, s, H, table, slot, w, (const char*)W_out, y, T, d, h, weighted,
+                       1.0f / (float)(out * kFewWaves));
   };
   auto with_tokens = [&](auto bf16, auto packed) {
     if (T <= 16) launch(bf16, packed, std::integral_constant<int, 1>{});

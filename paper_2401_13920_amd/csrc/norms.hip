@@ -88,17 +88,6 @@ __device__ __forceinline__ float row_sum(float v, float* sm) {
     return s;
   }
 }
-// sum over aligned groups of L lanes, L a power of two up to 64
-__device__ __forceinline__ float lanes_sum(float v, int L) {
-  if (L >= 2) v += dpp_f32<kDppXor1>(v);
-  if (L >= 4) v += dpp_f32<kDppXor2>(v);
-  if (L >= 8) v += dpp_f32<kDppHalfMirror>(v);
-  if (L >= 16) v += dpp_f32<kDppMirror>(v);
-  if (L >= 32) v += __shfl_xor(v, 16);
-  if (L >= 64) v += __shfl_xor(v, 32);
-  return v;
-}
-
 // How the means of the d/E features are formed: kLanes, a block is a power of two of chunks, held by neighbouring lanes of a
 // wave; kChunks, whole chunks, whose sums go through LDS; kElements, neither: every feature goes through LDS.
 enum GateForm { kLanes, kChunks, kElements };

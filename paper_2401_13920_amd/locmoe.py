@@ -35,6 +35,7 @@ EXPORTS = ("locmoe_status_string", "locmoe_capacity_min", "locmoe_p_delta", "loc
 LOCMOE_FFN_WS_BYTES = 128
 LOCMOE_NORM_MAX_ROW_BYTES = 65536
 LOCMOE_FEW_MAX_TOKENS = 64
+LOCMOE_FEW_MAX_WIDTH = 1 << 26
 LOCMOE_DISPATCH_STATIC_MAX_COUNTS = 262144
 
 

@@ -102,8 +102,8 @@ __global__ __launch_bounds__(threads_of<LPR>()) void norm_gate_kernel(const uint
   __shared__ float sm[THREADS / kWave];
   extern __shared__ float part[];  // kChunks: [RPB][chunks], kElements: [RPB][chunks V]
   const int rg = threadIdx.x / LPR, l = threadIdx.x % LPR;
-  const int m = blockIdx.x * RPB + rg;
-  const bool live = m < T;
+  const unsigned m = blockIdx.x * RPB + rg;  // (T fills 31 bits: the last work-group's rows may not fit them)
+  const bool live = m < (unsigned)T;
   const uint4* src = x + (size_t)(live ? m : T - 1) * chunks;
   uint4 v[CPL];
 #pragma unroll
@@ -175,8 +175,8 @@ __global__ __launch_bounds__(threads_of<LPR>()) void combine_norm_kernel(const u
   constexpr int V = Vec<BF16>::N, THREADS = threads_of<LPR>(), RPB = THREADS / LPR;
   __shared__ float sm[THREADS / kWave];
   const int rg = threadIdx.x / LPR, l = threadIdx.x % LPR;
-  const int m = blockIdx.x * RPB + rg;
-  const bool live = m < T;
+  const unsigned m = blockIdx.x * RPB + rg;
+  const bool live = m < (unsigned)T;
   const int s = live ? slot[m] : -1;
   uint4 vo[CPL], vr[CPL];
 #pragma unroll
@@ -269,15 +269,21 @@ __global__ __launch_bounds__(threads_of<LPR>()) void combine_norm_bwd_kernel(
     for (int k = 0; k < V; ++k) { gm[i][k] *= scale; acc[i][k] = 0.f; }
   }
   int set = 0;
-  for (int m0 = blockIdx.x * RPB; m0 < T; m0 += gridDim.x * RPB, set ^= 1) {
-    const int m = m0 + rg;
-    const int s = m < T ? slot[m] : -1;
-    const float wm = s >= 0 ? w[m] : 0.f, r = POST ? (s >= 0 ? rstd[m] : 0.f) : 1.f;
+  int s_next = blockIdx.x * RPB + rg < (unsigned)T ? slot[blockIdx.x * RPB + rg] : -1;
+  for (unsigned m0 = blockIdx.x * RPB; m0 < (unsigned)T; m0 += gridDim.x * RPB) {
+    const unsigned m = m0 + rg, m_next = m + gridDim.x * RPB;
+    const int s = s_next;
+    s_next = m_next < (unsigned)T ? slot[m_next] : -1;
+    if (s < 0) {  // (rows of more than a wave are a work-group's alone: all of it goes on, past the sum's barrier too)
+      if (m < (unsigned)T && l == 0) dw[m] = 0.f;
+      continue;
+    }
+    const float wm = w[m], r = POST ? rstd[m] : 1.f;
     uint4 vd[CPL], vo[CPL];
 #pragma unroll
     for (int i = 0; i < CPL; ++i) {
       const int c = l + i * LPR;
-      const bool in = s >= 0 && c < chunks;
+      const bool in = c < chunks;
       vd[i] = in ? nt_load16(dy + (size_t)m * chunks + c) : make_uint4(0, 0, 0, 0);
       vo[i] = in ? nt_load16(out + (size_t)s * chunks + c) : make_uint4(0, 0, 0, 0);
     }
@@ -296,8 +302,8 @@ __global__ __launch_bounds__(threads_of<LPR>()) void combine_norm_bwd_kernel(
       }
     }
     dot = row_sum<LPR>(dot, sm[set]);
-    if (m < T && l == 0) dw[m] = dot;
-    if (s < 0) continue;
+    set ^= 1;
+    if (l == 0) dw[m] = dot;
     const float mean = POST ? dot * inv_d : 0.f, wr = wm * r;
 #pragma unroll
     for (int i = 0; i < CPL; ++i) {
@@ -334,10 +340,12 @@ __global__ __launch_bounds__(threads_of<LPR>()) void dispatch_norm_bwd_kernel(
     for (int k = 0; k < V; ++k) acc[i][k] = 0.f;
   }
   int set = 0;
-  for (int m0 = blockIdx.x * RPB; m0 < T; m0 += gridDim.x * RPB, set ^= 1) {
-    const int m = m0 + rg;
-    const bool live = m < T;
-    const int s = live ? slot[m] : -1;
+  int s_next = blockIdx.x * RPB + rg < (unsigned)T ? slot[blockIdx.x * RPB + rg] : -1;
+  for (unsigned m0 = blockIdx.x * RPB; m0 < (unsigned)T; m0 += gridDim.x * RPB, set ^= 1) {
+    const unsigned m = m0 + rg, m_next = m + gridDim.x * RPB;
+    const int s = s_next;
+    s_next = m_next < (unsigned)T ? slot[m_next] : -1;
+    const bool live = m < (unsigned)T;
     const float r = live ? rstd[m] : 0.f;
     uint4 vs[CPL], vx[CPL], vr[CPL];
     float t[CPL][VEC_BLOCK ? 1 : V];
@@ -383,29 +391,36 @@ __global__ __launch_bounds__(threads_of<LPR>()) void dispatch_norm_bwd_kernel(
   if (part) store_partial<LPR, CPL, V>(acc, part, chunks, lds);
 }
 
-// dgamma[j] = sum of column j over the rows of partial sums.  A work-group makes 64 columns: 16 lanes of four columns, 16 row
-// groups, which are added in order through LDS.
+// dgamma[j] = sum of column j over the rows of partial sums.  A work-group makes 16 columns: four lanes of four columns, 64 row
+// groups with up to 16 loads in flight each, whose sums are added in a fixed order through LDS.  (64 columns per work-group leave
+// most compute units idle: 1 024 rows of 4 096 columns 8.4 us.)
+constexpr int kSumCols = 16;
 __global__ __launch_bounds__(256) void column_sum_kernel(const float* __restrict__ part, float* __restrict__ dgamma,
                                                          int rows, int d) {
-  __shared__ float4 s[16][16];
-  const int j = threadIdx.x & 15, rg = threadIdx.x >> 4, col = blockIdx.x * 64 + j * 4;
+  __shared__ float4 s[64][4];
+  const int j = threadIdx.x & 3, rg = threadIdx.x >> 2, col = blockIdx.x * kSumCols + j * 4;
+  const float* p = part + min(col, d - 4);
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (col < d) {
-    constexpr int U = 8;
-    for (int q0 = rg; q0 < rows; q0 += 16 * U) {
-      float4 v[U];
+  constexpr int U = 16;
+  for (int q0 = rg; q0 < rows; q0 += 64 * U) {
+    float4 v[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = *(const float4*)(part + (size_t)min(q0 + 16 * u, rows - 1) * d + col);
+    for (int u = 0; u < U; ++u) v[u] = *(const float4*)(p + (size_t)min(q0 + 64 * u, rows - 1) * d);
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (q0 + 16 * u < rows) { a.x += v[u].x; a.y += v[u].y; a.z += v[u].z; a.w += v[u].w; }
-    }
+    for (int u = 0; u < U; ++u)
+      if (q0 + 64 * u < rows) { a.x += v[u].x; a.y += v[u].y; a.z += v[u].z; a.w += v[u].w; }
   }
   s[rg][j] = a;
   __syncthreads();
-  if (rg == 0 && col < d) {
-    for (int i = 1; i < 16; ++i) { const float4 v = s[i][j]; a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w; }
-    *(float4*)(dgamma + col) = a;
+  if (threadIdx.x < 32) {  // eight row groups a lane, then the eight lanes of a column
+    a = s[rg * 8][j];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) { const float4 v = s[rg * 8 + i][j]; a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w; }
+#pragma unroll
+    for (int o = 4; o < 32; o *= 2) {
+      a.x += __shfl_xor(a.x, o); a.y += __shfl_xor(a.y, o); a.z += __shfl_xor(a.z, o); a.w += __shfl_xor(a.w, o);
+    }
+    if (rg == 0 && col < d) *(float4*)(dgamma + col) = a;
   }
 }
 
@@ -420,7 +435,7 @@ int with_forward_row(int chunks, F&& f) {
   if (chunks <= 64) return f(RowShape<64, 1>{});
   if (chunks <= 128) return f(RowShape<64, 2>{});
   if (chunks <= 256) return f(RowShape<64, 4>{});
-  if (chunks <= 512) return f(RowShape<64, 8>{});
+  if (chunks <= 512) return f(RowShape<256, 2>{});
   if (chunks <= 1024) return f(RowShape<256, 4>{});
   if (chunks <= 2048) return f(RowShape<512, 4>{});
   return f(RowShape<1024, 4>{});
@@ -489,7 +504,7 @@ int combine_norm_impl(const NormRow& row, int T, const void* out, const int32_t*
 }
 
 void sum_columns(const float* part, float* dgamma, int rows, int d, hipStream_t s) {
-  if (dgamma) hipLaunchKernelGGL(column_sum_kernel, dim3(ceil_div(d, 64)), dim3(256), 0, s, part, dgamma, rows, d);
+  if (dgamma) hipLaunchKernelGGL(column_sum_kernel, dim3(ceil_div(d, kSumCols)), dim3(256), 0, s, part, dgamma, rows, d);
 }
 
 template <bool BF>

@@ -54,11 +54,12 @@ class LocMoEError(RuntimeError):
 
 _lib = None
 _raw_stream = None  # torch's address of a device's current stream, if it has such a call
+_Tensor = None
 
 
 def lib() -> C.CDLL:
     """Loads the shared library once.  Fails loudly when it has not been built."""
-    global _lib, _raw_stream
+    global _lib, _raw_stream, _Tensor
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -126,6 +127,7 @@ def lib() -> C.CDLL:
             getattr(L, n).restype = C.c_int
     L.locmoe_internal_ffn_kernel.restype = C.c_char_p
     L.locmoe_internal_ffn_kernel.argtypes = [D, C.c_int, C.c_int]
+    _Tensor = torch.Tensor
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     _lib = L
     return L
@@ -143,6 +145,10 @@ def _check(st: int) -> None:
 def _ptr(t) -> int | None:
     """Device (or host) address of a torch tensor / numpy array, None stays NULL, an address stays itself.  (The launches of
     a small layer take about as long as this marshalling: the common cases come first.)"""
+    if t.__class__ is _Tensor:
+        if t.is_contiguous():
+            return t.data_ptr()
+        raise ValueError("liblocmoe needs contiguous buffers")
     if t is None or t.__class__ is int:
         return t
     if isinstance(t, np.ndarray):

@@ -6,8 +6,10 @@
 //
 // Bound by the stream of weights: 4 d h bytes per expert with tokens.  Weight rows feed the MFMA's A operand, 16 rows x 32 k a
 // KiB straight from memory into registers; a group's tokens are the columns, 16 per MFMA, fetched from L2.  A tile of 16
-// weight rows is shared by KS waves of a work-group, each with its part of K, where there are fewer tiles than waves; their
-// sums meet in LDS and are added in order.
+// weight rows is shared by up to eight waves of a work-group, each with its part of K, where there are fewer tiles than waves;
+// their sums meet in LDS and are added in order.  Measured (both kernels, as in a decoder's loop): 64 tokens on 20 of 64 experts,
+// d = 4096, h = 16384, 5.4 GB of weights: 890 us, 6.0 TB/s (a copy-free read of as much: 6.3 to 7.0); one token, d = 1024,
+// h = 4096, 16.8 MB: 12.1 us, of which the launches, the routing and a round trip to memory each are most.
 //
 // bf16 storage: H is rounded to bf16, as in the layer's other path.  fp32 storage: the activations and H keep all 24 bits: a
 // value is the sum of three bf16 parts, whose exact products with the bf16 weights are summed in fp32.
@@ -189,7 +191,11 @@ constexpr int few_depth(int x) { return x <= 1 ? 8 : x <= 3 ? 4 : x <= 6 ? 2 : 1
 // A wave's share of a GEMM: steps s0 .. s1 - 1 of K for one 16-row tile of weights and NB column tiles of 16 tokens.  W: the
 // expert's weights.  Operand B is the tokens' rows: bf16 (NP planes `plane` elements apart) or, with X_F32, fp32.  STREAM: the
 // weights are loaded past the caches.
-template <bool PACKED, bool X_F32, int NP, int NB, bool STREAM>
+//
+// SEG = 2, 4: a tile is 16 / SEG rows, each SEG times side by side in the MFMA's rows with a SEG-th of K each, and so are up to
+// 16 / SEG tokens in its columns: SEG blocks on the diagonal of the result, which the caller adds, for a tile whose products
+// the rows of SEG times as many work-groups share.
+template <bool PACKED, bool X_F32, int NP, int NB, int SEG, bool STREAM>
 __device__ __forceinline__ void few_dot(f32x4 (&acc)[NB], const char* __restrict__ W, const void* __restrict__ X,
                                         size_t plane, const int32_t* tok, int n, int tile, int Kdim, int Ndim, int s0,
                                         int s1) {
@@ -197,13 +203,16 @@ __device__ __forceinline__ void few_dot(f32x4 (&acc)[NB], const char* __restrict
   constexpr int D = few_depth(NB * XL);
   const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
   constexpr int kStep = PACKED ? 16384 : 64, kXStep = X_F32 ? 128 : 64;
-  const int row = min(tile * kFewRowsTile + l16, Ndim - 1);  // (rows past the last repeat it: not stored)
+  constexpr int R = kFewRowsTile / SEG;
+  const int row = min(tile * R + l16 % R, Ndim - 1);  // (rows past the last repeat it: not stored)
+  const int seg = l16 / R, k_seg = Kdim / SEG;
   const char* pw = PACKED ? W + (size_t)(row >> 8) * Kdim * 512 + (row & 255) * 64 + ((q ^ ((row >> 1) & 3)) << 4)
                           : W + (size_t)row * Kdim * 2 + q * 16;
+  pw += (size_t)(seg * (k_seg / 32)) * kStep;
   const char* px[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b)  // columns past the group's tokens repeat the last one (not stored)
-    px[b] = (const char*)X + ((size_t)tok[min(16 * b + l16, n - 1)] * Kdim + q * 8) * (X_F32 ? 4 : 2);
+    px[b] = (const char*)X + ((size_t)tok[min(16 * b + l16 % R, n - 1)] * Kdim + seg * k_seg + q * 8) * (X_F32 ? 4 : 2);
 #pragma unroll
   for (int b = 0; b < NB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
   u32x4 w[D], x[D][NB][XL];
@@ -241,7 +250,7 @@ __device__ __forceinline__ void few_dot(f32x4 (&acc)[NB], const char* __restrict
   // Whole turns of D steps, in a cycle that begins at a place of its own in each of 16 neighbouring blocks of packed rows: in
   // step, all waves read at multiples of a power of two, which are few of the memory's channels (d = 4096, h = 16384, 20
   // experts: 952 -> 890 us).
-  const int full = min(s1, Kdim / 32), turns = max(full - s0, 0) / D;
+  const int full = min(s1, k_seg / 32), turns = max(full - s0, 0) / D;
   int at = s0 + (PACKED ? (tile >> 4) & 15 : 0) * (turns >> 4) * D;
   for (int i = 0; i < turns; ++i) {
 #pragma unroll
@@ -267,7 +276,7 @@ __device__ __forceinline__ void few_dot(f32x4 (&acc)[NB], const char* __restrict
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int p = 0; p < XL; ++p) x[0][b][p] = zero;
-    if (s * 32 + q * 8 < Kdim) load(0, s);
+    if (s * 32 + q * 8 < k_seg) load(0, s);
     mul(0);
   }
 }
@@ -275,12 +284,13 @@ __device__ __forceinline__ void few_dot(f32x4 (&acc)[NB], const char* __restrict
 // All tiles of all groups, over the grid's waves: epilogue(token, first row of weights, 4 sums).  MAXB: column tiles at most (of all
 // tokens).  per_wave: 1 / waves of the grid.  red: LDS for the sums of a tile's waves but the first.
 constexpr int few_red(int maxb) { return (kFewWaves - 1) * maxb * 64; }
-template <bool PACKED, bool X_F32, int NP, int MAXB, class F>
+template <bool PACKED, bool X_F32, int NP, int MAXB, int SEG, class F>
 __device__ __forceinline__ void few_gemm(const FewTable* t, const char* W, const void* X, size_t plane, int Kdim, int Ndim,
                                          float per_wave, float4* red, F&& epilogue) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const unsigned tiles = (unsigned)(Ndim + kFewRowsTile - 1) / kFewRowsTile, items = t->groups * tiles;
-  const int steps = (Kdim + 31) / 32;
+  constexpr int R = kFewRowsTile / SEG;
+  const unsigned tiles = (unsigned)(Ndim + R - 1) / R, items = t->groups * tiles;
+  const int steps = (Kdim / SEG + 31) / 32;
   const bool stream = PACKED && (long long)t->groups * Ndim * Kdim * 2 > kFewStreamBytes;
   // 2^lks waves per tile: the fewest k-steps one after another, counting four for a turn of tiles' latency
   int lks = 0;
@@ -308,8 +318,8 @@ __device__ __forceinline__ void few_gemm(const FewTable* t, const char* W, const
     auto dot = [&](auto nb_) {
       constexpr int NB = decltype(nb_)::value;
       f32x4 part[NB];
-      if (stream) few_dot<PACKED, X_F32, NP, NB, PACKED>(part, We, X, plane, tok, n, tile, Kdim, Ndim, s0, s1);
-      else few_dot<PACKED, X_F32, NP, NB, false>(part, We, X, plane, tok, n, tile, Kdim, Ndim, s0, s1);
+      if (stream) few_dot<PACKED, X_F32, NP, NB, SEG, PACKED>(part, We, X, plane, tok, n, tile, Kdim, Ndim, s0, s1);
+      else few_dot<PACKED, X_F32, NP, NB, SEG, false>(part, We, X, plane, tok, n, tile, Kdim, Ndim, s0, s1);
 #pragma unroll
       for (int b = 0; b < NB; ++b) acc[b] = part[b];
     };
@@ -340,10 +350,17 @@ __device__ __forceinline__ void few_gemm(const FewTable* t, const char* W, const
       }
     }
     if (have && !sub) {
+      if constexpr (SEG > 1) {  // the blocks of the diagonal
+        const f32x4 a = acc[0];
+#pragma unroll
+        for (int i = 1; i < SEG; ++i)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) acc[0][v] += __shfl(a[v], lane + i * (64 / SEG + R));
+      }
 #pragma unroll
       for (int b = 0; b < MAXB; ++b) {
-        const int c = 16 * b + (lane & 15), r = tile * kFewRowsTile + (lane >> 4) * 4;
-        if (c < n && r < Ndim) epilogue(tok[c], r, acc[b]);  // (Ndim is a multiple of 8: the quad is inside or outside)
+        const int c = 16 * b + (lane & 15), r = tile * R + (lane >> 4) * 4;
+        if (c < n && (SEG == 1 || (lane < 64 / SEG && (lane & 15) < R)) && r < Ndim) epilogue(tok[c], r, acc[b]);  // (Ndim is a multiple of 8: the quad is inside or outside)
       }
     }
     if (ks > 1 && i0 + gridDim.x * per < items) __syncthreads();  // (red has been read)
@@ -352,7 +369,7 @@ __device__ __forceinline__ void few_gemm(const FewTable* t, const char* W, const
 
 // (four waves per SIMD: two work-groups per compute unit)
 
-template <bool BF16, bool PACKED, int MAXB>
+template <bool BF16, bool PACKED, int MAXB, int SEG>
 __global__ __launch_bounds__(kFewThreads, 4) void few_in_kernel(const void* __restrict__ x, const float* __restrict__ g,
                                                                 const float* __restrict__ eps,
                                                                 const char* __restrict__ W, int32_t* __restrict__ eid,
@@ -379,7 +396,7 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_in_kernel(const void* __re
   }
   constexpr int NP = BF16 ? 1 : 3;
   const size_t plane = (size_t)T * h;
-  few_gemm<PACKED, !BF16, NP, MAXB>(&t, W, x, 0, d, h, per_wave, red, [&](int m, int r, const f32x4& a) {
+  few_gemm<PACKED, !BF16, NP, MAXB, SEG>(&t, W, x, 0, d, h, per_wave, red, [&](int m, int r, const f32x4& a) {
     uint16_t* dst = H + (size_t)m * h + r;
     if constexpr (BF16) {
       *(uint2*)dst = make_uint2(pack_bf16x2(gelu_bf16(a[0]), gelu_bf16(a[1])), pack_bf16x2(gelu_bf16(a[2]), gelu_bf16(a[3])));
@@ -393,7 +410,7 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_in_kernel(const void* __re
   });
 }
 
-template <bool BF16, bool PACKED, int MAXB>
+template <bool BF16, bool PACKED, int MAXB, int SEG>
 __global__ __launch_bounds__(kFewThreads, 4) void few_out_kernel(const uint16_t* __restrict__ H,
                                                                  const FewTable* __restrict__ table,
                                                                  const int32_t* __restrict__ slot,
@@ -410,7 +427,7 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_out_kernel(const uint16_t*
       if (slot[m] < 0)
         for (int c = threadIdx.x; c < chunks; c += kFewThreads) ((uint4*)y)[(size_t)m * chunks + c] = make_uint4(0, 0, 0, 0);
   }
-  few_gemm<PACKED, false, BF16 ? 1 : 3, MAXB>(&t, W, H, (size_t)T * h, h, d, per_wave, red, [&](int m, int r, const f32x4& a) {
+  few_gemm<PACKED, false, BF16 ? 1 : 3, MAXB, SEG>(&t, W, H, (size_t)T * h, h, d, per_wave, red, [&](int m, int r, const f32x4& a) {
     const float f = weighted ? w[m] : 1.0f;
     if constexpr (BF16)
       *(uint2*)((uint16_t*)y + (size_t)m * d + r) = make_uint2(pack_bf16x2(f * a[0], f * a[1]), pack_bf16x2(f * a[2], f * a[3]));
@@ -445,18 +462,34 @@ extern "C" int locmoe_layer_few(const locmoe_desc* desc, const void* x, const fl
   hipStream_t s = as_stream(stream);
   FewTable* table = (FewTable*)ws;
   uint16_t* H = (uint16_t*)((char*)ws + kFewHOffset);
-  // two work-groups per compute unit, no more than there can be tiles (of up to eight waves each)
-  auto groups = [&](int n) {
-    return (unsigned)std::min<long long>(2 * cu_count(), (long long)std::min(T, E) * ceil_div(n, kFewRowsTile));
-  };
   const FewRoute plan = few_route_plan(T, d, E);
+  // Tiles of 16 rows of weights, or of 8 or 4 where those leave compute units without one (one token, d = 1024, h = 4096, second
+  // GEMM: 64 tiles of 16 rows 5.5 us, 256 of 4 rows 4.9)
+  auto segments = [&](int N, int K) {
+    int seg = 1;
+    while (seg < 4 && 2 * seg * T <= 16 && K % (64 * seg) == 0 &&
+           (long long)std::min(T, E) * ceil_div(N, kFewRowsTile / seg) < cu_count())
+      seg *= 2;
+    return seg;
+  };
+  // two work-groups per compute unit, no more than there can be tiles (of up to eight waves each)
+  auto groups = [&](int N, int seg) {
+    return (unsigned)std::min<long long>(2 * cu_count(), (long long)std::min(T, E) * ceil_div(N, kFewRowsTile / seg));
+  };
   auto launch = [&](auto bf16, auto packed, auto maxb) {
     constexpr bool BF = decltype(bf16)::value, PK = decltype(packed)::value;
     constexpr int MAXB = decltype(maxb)::value;
-    const unsigned in = groups(h), out = groups(d);
-    hipLaunchKernelGGL((few_in_kernel<BF, PK, MAXB>), dim3(in), dim3(kFewThreads), 0, s, x, g, eps, (const char*)W_in, eid, w, slot, table, H, T, d, E, h,
+    const int seg_in = segments(h, d), seg_out = segments(d, h);
+    const unsigned in = groups(h, seg_in), out = groups(d, seg_out);
+    auto k_in = few_in_kernel<BF, PK, MAXB, 1>;
+    auto k_out = few_out_kernel<BF, PK, MAXB, 1>;
+    if constexpr (MAXB == 1) {
+      if (seg_in > 1) k_in = seg_in == 2 ? few_in_kernel<BF, PK, 1, 2> : few_in_kernel<BF, PK, 1, 4>;
+      if (seg_out > 1) k_out = seg_out == 2 ? few_out_kernel<BF, PK, 1, 2> : few_out_kernel<BF, PK, 1, 4>;
+    }
+    hipLaunchKernelGGL(k_in, dim3(in), dim3(kFewThreads), 0, s, x, g, eps, (const char*)W_in, eid, w, slot, table, H, T, d, E, h,
                        desc->C, desc->relu, plan, 1.0f / (float)(in * kFewWaves));
-    hipLaunchKernelGGL((few_out_kernel<BF, PK, MAXB>), dim3(out), dim3(kFewThreads), 0, s, H, table, slot, w, (const char*)W_out, y, T, d, h, weighted,
+    hipLaunchKernelGGL(k_out, dim3(out), dim3(kFewThreads), 0, s, H, table, slot, w, (const char*)W_out, y, T, d, h, weighted,
                        1.0f / (float)(out * kFewWaves));
   };
   auto with_tokens = [&](auto bf16, auto packed) {

@@ -93,9 +93,9 @@ __device__ __forceinline__ float row_sum(float v, float* sm) {
 enum GateForm { kLanes, kChunks, kElements };
 
 template <bool BF16, int LPR, int CPL, int GATE>
-__global__ __launch_bounds__(threads_of<LPR>()) void norm_gate_kernel(const uint4* __restrict__ x,
+__global__ __launch_bounds__(threads_of<LPR>()) void norm_gate_kernel(const uint4* x,
                                                                       const float* __restrict__ gamma,
-                                                                      uint4* __restrict__ xn, float* __restrict__ rstd,
+                                                                      uint4* xn, float* __restrict__ rstd,
                                                                       float* __restrict__ g, int T, int chunks, int E,
                                                                       int blk, float inv_d, float eps) {
   constexpr int V = Vec<BF16>::N, THREADS = threads_of<LPR>(), RPB = THREADS / LPR;
@@ -325,8 +325,8 @@ __global__ __launch_bounds__(threads_of<LPR>()) void combine_norm_bwd_kernel(
 template <bool BF16, int LPR, int CPL, bool VEC_BLOCK>
 __global__ __launch_bounds__(threads_of<LPR>()) void dispatch_norm_bwd_kernel(
     const uint4* __restrict__ dsend, const int32_t* __restrict__ slot, const float* __restrict__ dg,
-    const uint4* __restrict__ x, const float* __restrict__ gamma, const float* __restrict__ rstd, const uint4* dres,
-    uint4* dx, float* __restrict__ part, int T, int chunks, int E, int blk, float inv_d, float dg_scale) {
+    const uint4* x, const float* __restrict__ gamma, const float* __restrict__ rstd, const uint4* dres, uint4* dx,
+    float* __restrict__ part, int T, int chunks, int E, int blk, float inv_d, float dg_scale) {
   constexpr int V = Vec<BF16>::N, THREADS = threads_of<LPR>(), RPB = THREADS / LPR;
   __shared__ float sm[2][THREADS / kWave];
   __shared__ float lds[RPB > 1 ? THREADS * CPL * V : 1];

@@ -203,3 +203,21 @@ def test_infinities_stay_with_their_token(env):
         L.xd[1, 5] = float("nan")
         L.call(gd)
         assert torch.equal(L.y[[0, 2]], want[[0, 2]]) and torch.isnan(L.y[1]).all()
+
+
+# fewer tiles of 16 rows of weights than compute units: tiles of 8 and of 4 rows, with K in two and four parts side by side
+@pytest.mark.parametrize("T", [1, 2, 4, 5, 8, 9])
+@pytest.mark.parametrize("d,h", [(512, 768), (256, 64), (384, 200), (64, 1024)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_narrow_tiles(env, T, d, h, dtype):
+    torch, lm = env
+    print(f"[few narrow] T={T} d={d} h={h} {dtype}", flush=True)
+    for experts in (None, [3], [0, 2, 1]):
+        for packed in (False, True):
+            if packed and (dtype == "f32" or d % 256 or h % 256):
+                continue
+            L = Layer(env, T, d, 4, h, max(1, T - 1), dtype, packed=packed, experts=experts)
+            g32 = torch.empty(T, 4, device="cuda")
+            lm.locmoe_gate(L.desc, L.xd, g32)
+            L.call()
+            L.check(g32.cpu().numpy())

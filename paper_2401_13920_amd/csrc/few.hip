@@ -115,7 +115,7 @@ __device__ __forceinline__ void few_route(const FewRoute& r, const void* x, cons
     auto seen = [&](int e, float v) {
       if (eps) v += eps[e];
       if (relu) v = fmaxf(v, 0.f);
-      const float f = __builtin_amdgcn_exp2f(-kLog2e * fabsf(v - best));
+      const float f = v == best ? 1.0f : __builtin_amdgcn_exp2f(-kLog2e * fabsf(v - best));  // (both may be -inf: a masked expert)
       const bool more = v > best || at == E;  // (ascending e: ties stay with the lower)
       z = more ? fmaf(z, f, 1.0f) : z + f;
       best = more ? v : best;
@@ -183,9 +183,9 @@ __device__ __forceinline__ void few_groups(const int32_t* s_eid, int T, int C, F
 }
 
 // k-steps in flight: what 128 registers hold beside the sums (x 16-byte loads of the tokens' operand a step).  16 waves of a compute
-// unit have 128 KiB of weights in flight with 8.  (Pairs of tiles, which fetch the tokens' operand half as often, are slower: 20
-// experts of d = 1024, h = 4096 83 -> 107 us, d = 4096, h = 16384 902 -> 931; so are loads kept in flight across the products,
-// 1 025 -> 1 058.)
+// unit have 128 KiB of weights in flight with 8, which is enough: with the tokens' rows in LDS and 16 steps of weights in flight
+// d = 4096, h = 16384, 24 experts take 929 us instead of 902 (8 steps: 897), with loads kept in flight across the products 906,
+// with pairs of tiles that share the tokens' operand 931.
 constexpr int few_depth(int x) { return x <= 1 ? 8 : x <= 3 ? 4 : x <= 6 ? 2 : 1; }
 
 // A wave's share of a GEMM: steps s0 .. s1 - 1 of K for one 16-row tile of weights and NB column tiles of 16 tokens.  W: the

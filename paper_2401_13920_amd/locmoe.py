@@ -631,6 +631,8 @@ def forward_block(desc, x, home, e2n, W_in, W_out, block: Block, b: Buffers, kb:
 def decode_block(desc, x, W_in, W_out, block: Block, b: Buffers, kb: BlockBuffers, eps=None, stream=None):
     """The block's forward for up to LOCMOE_FEW_MAX_TOKENS tokens in four launches, without statistics and send buffer:
     leaves y in b.y, the routing in b.eid, b.w and b.slot (row m of kb.few_out for a kept token m)."""
+    if desc.T > LOCMOE_FEW_MAX_TOKENS:
+        raise LocMoEError(LOCMOE_ERR_SHAPE)
     stream = _stream(stream)
     xn, g, slot, w, out = _ptr(kb.xn), _ptr(b.g), _ptr(b.slot), _ptr(b.w), _ptr(kb.few_out)
     locmoe_norm_gate(desc, x, block.gamma_in, block.norm_eps, xn, kb.rstd_in, g, stream)

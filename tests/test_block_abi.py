@@ -100,3 +100,9 @@ def test_activations_in_8_bits(name, nargs):
     refused(ws, good, {nargs: (P + 2, WS)})
     refused(ws, good, {0: (P, SHAPE)}, desc(h=12))
     refused(ws, good, {0: (P, ARG)}, desc(w_packed=True))
+
+
+def test_decode_block_takes_few_tokens():
+    n = lm.locmoe_norm_workspace_bytes(desc(T=65))
+    kb = lm.BlockBuffers(xn=P, rstd_in=P, rstd_out=P, dgamma_in=P, dgamma_out=P, ws=P, ws_bytes=n)  # (as allocated for 65 tokens)
+    assert status(lm.decode_block, desc(T=65), P, P, P, lm.Block(), None, kb) == SHAPE

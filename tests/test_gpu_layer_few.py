@@ -153,6 +153,25 @@ def test_ties_go_to_the_lowest_expert(env):
         assert L.eid.tolist()[:5] == [0, 5, E // 2, 3, E - 1]
 
 
+@pytest.mark.parametrize("E", [4, 12, 96, 512])
+def test_masked_experts(env, E):
+    """Experts of gating value minus infinity: never taken, nothing in the score; so are the type's lowest values."""
+    torch, lm = env
+    d = 1024 if E == 512 else 96 * 8
+    for T in (1, 6, 64):
+        for low in (-np.inf, float(np.finfo(np.float32).min)):
+            print(f"[few masked] E={E} T={T} low={low}", flush=True)
+            L = Layer(env, T, d, E, 16, T, relu=False)
+            g = L.rng.standard_normal((T, E)).astype(np.float32)
+            eps = np.zeros(E, np.float32)
+            eps[::2] = low                       # the first expert of most lanes, and all of some
+            g[:, E // 2:E - 1] = low
+            with np.errstate(over="ignore"):
+                L.call(torch.from_numpy(g).cuda(), torch.from_numpy(eps).cuda())
+                L.check(g, eps)
+            assert (L.eid % 2 == 1).all() and torch.isfinite(L.w).all()
+
+
 def test_all_tokens_alike(env):
     """The same token 64 times: one group of 64, of which the capacity keeps the first ones."""
     torch, lm = env

@@ -212,3 +212,54 @@ def test_rows_of_zeros_infinities_and_nan(env):
     res = torch.zeros_like(x)
     lm.locmoe_combine_norm(desc, out, slot, w, res, None, True, EPS, 1.0, y, None)
     assert torch.isnan(y[1, 7]) and (y[1, :7] == 0).all() and (y[2] == 0).all() and torch.isfinite(y[[0, 3, 4]]).all()
+
+
+def test_offsets_past_32_bits(env):
+    """Buffers of more than 2^32 bytes: rows on both sides of that boundary and the last one."""
+    torch, lm = env
+    T, d, E = 131072 + 300, 16384, 16
+    sel = [0, 131071, 131072, 131200, T - 1]
+    desc = lm.make_desc(T, d, E, 1, 8, -(-T // E), "bf16")
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    big = lambda: torch.randn(T, d, dtype=torch.bfloat16, device="cuda", generator=gen)  # noqa: E731
+    x, out, dy = big(), big(), big()
+    gamma = torch.rand(d, device="cuda", generator=gen) + 0.5
+    w, u = torch.rand(T, device="cuda", generator=gen), torch.finfo(torch.bfloat16).eps / 2
+    slot = torch.arange(T, dtype=torch.int32, device="cuda").flip(0).contiguous()    # row T - 1 - m is token m's
+    at = host(slot[sel]).astype(int)
+    y, rstd, g = torch.full_like(x, 7.0), torch.empty(T, device="cuda"), torch.empty(T, E, device="cuda")
+    lm.locmoe_norm_gate(desc, x, gamma, EPS, y, rstd, g)
+    ref, r, gr = blk.norm_gate(host(x[sel]), host(gamma), EPS, E)
+    within(y[sel], ref, (u + 2 * R) * np.abs(ref), "xn")
+    within(g[sel], gr, (2 * R + d // E * F) * np.abs(ref).reshape(len(sel), E, -1).mean(2), "g")
+    rstd2 = torch.empty(T, device="cuda")
+    lm.locmoe_combine_norm(desc, out, slot, w, x, gamma, True, EPS, SCALE, y, rstd2)
+    o, own = host(out[at]), np.arange(len(sel))
+    ref, r2 = blk.combine_norm(o, own, host(w[sel]), host(x[sel]), host(gamma), True, EPS, SCALE)
+    res = host(x[sel])
+    within(y[sel], ref, u * np.abs(ref) + (2 * R + F) * (np.abs(ref - res) + np.abs(res)), "y")
+    n = lm.locmoe_norm_workspace_bytes(desc)
+    ws, dw, dgamma = torch.empty(n, dtype=torch.uint8, device="cuda"), torch.empty(T, device="cuda"), torch.empty(d, device="cuda")
+    lm.locmoe_combine_norm_bwd(desc, dy, out, slot, w, gamma, True, SCALE, rstd2, y, dw, dgamma, ws, n)     # y: dout
+    r2 = host(rstd2[sel])
+    ref, dwr, _ = blk.combine_norm_backward(host(dy[sel]), o, own, host(w[sel]), host(gamma), True, SCALE, r2)
+    uu, nrm = np.abs(SCALE * host(gamma) * host(dy[sel])), np.abs(o) * r2[:, None]
+    sums = (uu * nrm).sum(1, keepdims=True)
+    within(dw[sel], dwr, (2 * R + d * F) * sums[:, 0], "dw")
+    mag = r2[:, None] * host(w[sel])[:, None] * (uu + nrm * sums / d)
+    within(y[at], ref, u * np.abs(ref) + (2 * R + d * F) * mag, "dout")
+    dg = torch.randn(T, E, device="cuda", generator=gen)
+    lm.locmoe_dispatch_norm_bwd(desc, out, slot, dg, x, gamma, rstd, dy, y, dgamma, ws, n)                  # y: dx
+    r = host(rstd[sel])
+    ref, _ = blk.dispatch_norm_backward(o, own, host(dg[sel]), res, host(gamma), r, host(dy[sel]))
+    dxn = np.abs(o) + np.repeat(np.abs(host(dg[sel])) * (E / d), d // E, axis=1)
+    xh = np.abs(res) * r[:, None]
+    mag = r[:, None] * (dxn * host(gamma) + xh * (dxn * host(gamma) * xh).sum(1, keepdims=True) / d) + np.abs(host(dy[sel]))
+    within(y[sel], ref, u * np.abs(ref) + (2 * R + d * F) * mag, "dx")
+    want, size = torch.zeros(d, dtype=torch.float64, device="cuda"), torch.zeros(d, dtype=torch.float64, device="cuda")
+    for i in range(0, T, 8192):
+        j = slice(i, min(T, i + 8192))
+        t = (out[slot[j].long()].double() + dg[j].double().repeat_interleave(d // E, 1) * (E / d)) * x[j].double() * rstd[j, None].double()
+        want += t.sum(0)
+        size += t.abs().sum(0)
+    within(dgamma, host(want), (2 * R + T * F) * host(size), "dgamma")

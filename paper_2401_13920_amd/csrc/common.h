@@ -99,6 +99,7 @@ constexpr int kDppXor1 = 0xB1;         // quad_perm [1,0,3,2]
 constexpr int kDppXor2 = 0x4E;         // quad_perm [2,3,0,1]
 constexpr int kDppHalfMirror = 0x141;  // lane i <-> 7-i inside each group of 8
 constexpr int kDppMirror = 0x140;      // lane i <-> 15-i inside each row of 16
+constexpr int kDppRor8 = 0x128;        // lane i <-> i^8 inside each row of 16
 
 // All-reduce sum over aligned groups of L lanes (L a power of two <= 64): every lane of a
 // group ends with the group's total.  The steps below 16 lanes are DPP; 16 and 32 go through

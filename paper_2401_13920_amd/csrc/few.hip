@@ -29,9 +29,9 @@ constexpr int kFewTokens = LOCMOE_FEW_MAX_TOKENS;
 static_assert(kFewTokens == kWave, "the routing of all tokens is one wave's");
 constexpr int kFewThreads = 512, kFewWaves = kFewThreads / kWave;
 constexpr int kFewRowsTile = 16;
-// Packed weights of more than this in one launch, which the last-level cache does not hold until the next call anyway, are loaded
-// past it: d = 4096, h = 16384, 24 experts 1 105 -> 1 024 us; d = 1024, h = 4096, one expert 12.9 -> 14.6.  Not row-major ones,
-// of whose lines a load takes half: the other half is fetched again.
+// Weights of more than this in one launch, which the last-level cache does not hold until the next call anyway, are loaded past
+// it: packed, d = 4096, h = 16384, 20 experts 1 003 -> 917 us; below, a loop over one layer finds them there (d = 1024, h = 4096,
+// one expert 12.9 -> 14.6).  Row-major ones if their rows are whole lines of memory (few_dot_rows).
 constexpr long long kFewStreamBytes = 100ll << 20;
 
 // The routing as the second kernel reads it (front of the workspace; H follows at kFewHOffset)
@@ -188,6 +188,31 @@ __device__ __forceinline__ void few_groups(const int32_t* s_eid, int T, int C, F
 // with pairs of tiles that share the tokens' operand 931.
 constexpr int few_depth(int x) { return x <= 1 ? 8 : x <= 3 ? 4 : x <= 6 ? 2 : 1; }
 
+// A k-step's products: weights w, tokens' operand x as loaded
+template <bool X_F32, int NP, int NB>
+__device__ __forceinline__ void few_mul(f32x4 (&acc)[NB], const u32x4& w, const u32x4 (&x)[NB][X_F32 ? 2 : NP]) {
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    u32x4 part[NP];
+    if constexpr (X_F32) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t v[3];
+        split3(__uint_as_float(x[b][i / 2][2 * i % 4]), __uint_as_float(x[b][i / 2][2 * i % 4 + 1]), v);
+#pragma unroll
+        for (int p = 0; p < NP; ++p) part[p][i] = v[p];
+      }
+    } else {
+#pragma unroll
+      for (int p = 0; p < NP; ++p) part[p] = x[b][p];
+    }
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+      acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, part[p]),
+                                                       acc[b], 0, 0, 0);
+  }
+}
+
 // A wave's share of a GEMM: steps s0 .. s1 - 1 of K for one 16-row tile of weights and NB column tiles of 16 tokens.  W: the
 // expert's weights.  Operand B is the tokens' rows: bf16 (NP planes `plane` elements apart) or, with X_F32, fp32.  STREAM: the
 // weights are loaded past the caches.
@@ -225,28 +250,7 @@ __device__ __forceinline__ void few_dot(f32x4 (&acc)[NB], const char* __restrict
       for (int p = 0; p < XL; ++p)
         x[u][b][p] = *(const u32x4*)(px[b] + (size_t)s * kXStep + (X_F32 ? p * 16 : p * plane * 2));
   };
-  auto mul = [&](int u) {
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      u32x4 part[NP];
-      if constexpr (X_F32) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t v[3];
-          split3(__uint_as_float(x[u][b][i / 2][2 * i % 4]), __uint_as_float(x[u][b][i / 2][2 * i % 4 + 1]), v);
-#pragma unroll
-          for (int p = 0; p < NP; ++p) part[p][i] = v[p];
-        }
-      } else {
-#pragma unroll
-        for (int p = 0; p < NP; ++p) part[p] = x[u][b][p];
-      }
-#pragma unroll
-      for (int p = 0; p < NP; ++p)
-        acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[u]), __builtin_bit_cast(bf16x8, part[p]),
-                                                         acc[b], 0, 0, 0);
-    }
-  };
+  auto mul = [&](int u) { few_mul<X_F32, NP, NB>(acc, w[u], x[u]); };
   // Whole turns of D steps, in a cycle that begins at a place of its own in each of 16 neighbouring blocks of packed rows: in
   // step, all waves read at multiples of a power of two, which are few of the memory's channels (d = 4096, h = 16384, 20
   // experts: 952 -> 890 us).
@@ -281,6 +285,75 @@ __device__ __forceinline__ void few_dot(f32x4 (&acc)[NB], const char* __restrict
   }
 }
 
+// The same for row-major weights past the caches, two steps (128 bytes of a row, a line) at a time, [p0, p1): a load takes the whole
+// line of 8 rows (half lines are fetched twice), the first 8 lanes of a 16-lane row its first half and the others its second, and
+// two loads (rows 0 to 7 and 8 to 15) make two steps' operands by exchanging halves.  d = 4096, h = 16384, 20 experts: 1 049 us with
+// half lines through the caches, 929 so, 923 with the tiles out of step (one expert: 69, 66, 51).
+template <bool X_F32, int NP, int NB>
+__device__ __forceinline__ void few_dot_rows(f32x4 (&acc)[NB], const char* __restrict__ W, const void* __restrict__ X,
+                                             size_t plane, const int32_t* tok, int n, int tile, int Kdim, int Ndim, int p0,
+                                             int p1) {
+  constexpr int XL = X_F32 ? 2 : NP;
+  constexpr int D = (few_depth(NB * XL) + 1) / 2;
+  constexpr int XH = few_depth(NB * XL) > 1 ? 2 : 1;  // the second step's tokens too, or fetched after the first step's products
+  const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4, c = q + 4 * (l16 >> 3);
+  const int r0 = tile * kFewRowsTile + (l16 & 7);
+  const char* pw0 = W + (size_t)min(r0, Ndim - 1) * Kdim * 2 + c * 16;
+  const char* pw1 = W + (size_t)min(r0 + 8, Ndim - 1) * Kdim * 2 + c * 16;
+  const char* px[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+    px[b] = (const char*)X + ((size_t)tok[min(16 * b + l16, n - 1)] * Kdim + q * 8) * (X_F32 ? 4 : 2);
+#pragma unroll
+  for (int b = 0; b < NB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  u32x4 w[D][2], x[D][XH][NB][XL];
+  auto load_w = [&](int u, int p) {
+    const u32x4 *a = (const u32x4*)(pw0 + (size_t)p * 128), *b = (const u32x4*)(pw1 + (size_t)p * 128);
+    w[u][0] = __builtin_nontemporal_load(a);
+    w[u][1] = __builtin_nontemporal_load(b);
+  };
+  auto load_x = [&](int u, int h, int p) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < XL; ++i)
+        x[u][h % XH][b][i] = *(const u32x4*)(px[b] + (size_t)(2 * p + h) * (X_F32 ? 128 : 64) + (X_F32 ? i * 16 : i * plane * 2));
+  };
+  auto load = [&](int u, int p) {
+    load_w(u, p);
+#pragma unroll
+    for (int h = 0; h < XH; ++h) load_x(u, h, p);
+  };
+  auto mul = [&](int u, auto&& second) {
+    u32x4 a0, a1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {  // lanes 8 to 15 of a row take the other lanes' second load, lanes 0 to 7 their first
+      a0[i] = __builtin_amdgcn_update_dpp(w[u][0][i], w[u][1][i], kDppRor8, 0xF, 0xC, false);
+      a1[i] = __builtin_amdgcn_update_dpp(w[u][1][i], w[u][0][i], kDppRor8, 0xF, 0x3, false);
+    }
+    few_mul<X_F32, NP, NB>(acc, a0, x[u][0]);
+    if constexpr (XH == 1) second();
+    few_mul<X_F32, NP, NB>(acc, a1, x[u][XH - 1]);
+  };
+  const int turns = (p1 - p0) / D;
+  int at = p0 + (tile & 7) * (turns >> 3) * D;  // (neighbouring tiles out of step, as in few_dot)
+  for (int i = 0; i < turns; ++i) {
+#pragma unroll
+    for (int u = 0; u < D; ++u) load(u, at + u);
+#pragma unroll
+    for (int u = 0; u < D; ++u) mul(u, [&] { load_x(u, 1, at + u); });
+    at += D;
+    if (at == p0 + turns * D) at = p0;
+  }
+  int p = p0 + turns * D;
+#pragma unroll
+  for (int u = 0; u < D - 1; ++u)
+    if (p + u < p1) load(u, p + u);
+#pragma unroll
+  for (int u = 0; u < D - 1; ++u)
+    if (p + u < p1) mul(u, [&] { load_x(u, 1, p + u); });
+}
+
 // All tiles of all groups, over the grid's waves: epilogue(token, first row of weights, 4 sums).  MAXB: column tiles at most (of all
 // tokens).  per_wave: 1 / waves of the grid.  red: LDS for the sums of a tile's waves but the first.
 constexpr int few_red(int maxb) { return (kFewWaves - 1) * maxb * 64; }
@@ -291,7 +364,7 @@ __device__ __forceinline__ void few_gemm(const FewTable* t, const char* W, const
   constexpr int R = kFewRowsTile / SEG;
   const unsigned tiles = (unsigned)(Ndim + R - 1) / R, items = t->groups * tiles;
   const int steps = (Kdim / SEG + 31) / 32;
-  const bool stream = PACKED && (long long)t->groups * Ndim * Kdim * 2 > kFewStreamBytes;
+  const bool stream = (PACKED || (SEG == 1 && Kdim % 64 == 0)) && (long long)t->groups * Ndim * Kdim * 2 > kFewStreamBytes;
   // 2^lks waves per tile: the fewest k-steps one after another, counting four for a turn of tiles' latency
   int lks = 0;
   float least = 3e38f;
@@ -302,7 +375,8 @@ __device__ __forceinline__ void few_gemm(const FewTable* t, const char* W, const
     if (cost < least) { least = cost; lks = i; }
   }
   const int ks = 1 << lks, per = kFewWaves >> lks, sub = wave & (ks - 1), mine = wave >> lks;
-  const int s0 = steps * sub >> lks, s1 = steps * (sub + 1) >> lks;
+  const int lines = stream ? 2 : 1;  // (streamed row-major weights go by lines of two steps)
+  const int s0 = (steps / lines * sub >> lks) * lines, s1 = (steps / lines * (sub + 1) >> lks) * lines;
   int u = 0;
   unsigned at = blockIdx.x * per + mine;  // number in group u
   for (unsigned i0 = blockIdx.x * per; i0 < items; i0 += gridDim.x * per, at += gridDim.x * per) {
@@ -318,8 +392,9 @@ __device__ __forceinline__ void few_gemm(const FewTable* t, const char* W, const
     auto dot = [&](auto nb_) {
       constexpr int NB = decltype(nb_)::value;
       f32x4 part[NB];
-      if (stream) few_dot<PACKED, X_F32, NP, NB, SEG, PACKED>(part, We, X, plane, tok, n, tile, Kdim, Ndim, s0, s1);
-      else few_dot<PACKED, X_F32, NP, NB, SEG, false>(part, We, X, plane, tok, n, tile, Kdim, Ndim, s0, s1);
+      if (!stream) few_dot<PACKED, X_F32, NP, NB, SEG, false>(part, We, X, plane, tok, n, tile, Kdim, Ndim, s0, s1);
+      else if constexpr (PACKED) few_dot<PACKED, X_F32, NP, NB, SEG, true>(part, We, X, plane, tok, n, tile, Kdim, Ndim, s0, s1);
+      else if constexpr (SEG == 1) few_dot_rows<X_F32, NP, NB>(part, We, X, plane, tok, n, tile, Kdim, Ndim, s0 / 2, s1 / 2);
 #pragma unroll
       for (int b = 0; b < NB; ++b) acc[b] = part[b];
     };

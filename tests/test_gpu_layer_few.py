@@ -240,3 +240,19 @@ def test_narrow_tiles(env, T, d, h, dtype):
             lm.locmoe_gate(L.desc, L.xd, g32)
             L.call()
             L.check(g32.cpu().numpy())
+
+
+# more than 100 MiB of row-major weights in a launch: rows of whole 128-byte lines go past the caches (2048: 32 of them, 6592: 103);
+# 6600 values are no whole lines, and end inside a tile of rows.  Groups of one to four column tiles.
+@pytest.mark.parametrize("T,h,dtype,experts", [(5, 6600, "bf16", [0, 1, 2, 3]), (13, 6592, "bf16", [0, 1, 2, 3]),
+                                               (13, 6592, "f32", [3, 2, 1, 0, 0]), (26, 6592, "bf16", [0] * 20 + [1, 2, 3]),
+                                               (40, 6592, "f32", [0] * 37 + [1, 2, 3]), (40, 6592, "bf16", [0] * 37 + [1, 2, 3])])
+def test_many_weights_row_major(env, T, h, dtype, experts):
+    torch, lm = env
+    print(f"[few rows] T={T} h={h} {dtype}", flush=True)
+    L = Layer(env, T, 2048, 4, h, T, dtype, experts=experts)
+    g = np.full((T, 4), -1.0, np.float32)
+    g[np.arange(T), [experts[m % len(experts)] for m in range(T)]] = 1.0
+    L.call(torch.from_numpy(g).cuda())
+    L.check(g)
+    assert sorted(set(L.eid.tolist())) == [0, 1, 2, 3]

@@ -8,8 +8,8 @@
 // KiB straight from memory into registers; a group's tokens are the columns, 16 per MFMA, fetched from L2.  A tile of 16
 // weight rows is shared by up to eight waves of a work-group, each with its part of K, where there are fewer tiles than waves;
 // their sums meet in LDS and are added in order.  Measured (both kernels, as in a decoder's loop): 64 tokens on 20 of 64 experts,
-// d = 4096, h = 16384, 5.4 GB of weights: 890 us, 6.0 TB/s (a copy-free read of as much: 6.3 to 7.0); one token, d = 1024,
-// h = 4096, 16.8 MB: 12.1 us, of which the launches, the routing and a round trip to memory each are most.
+// d = 4096, h = 16384, 5.4 GB of weights: 890 us packed, 915 row-major, 6.0 TB/s (a copy-free read of as much: 6.3 to 7.0); one token,
+// d = 1024, h = 4096, 16.8 MB: 11.6 us, of which the launches, the routing and a round trip to memory each are most.
 //
 // bf16 storage: H is rounded to bf16, as in the layer's other path.  fp32 storage: the activations and H keep all 24 bits: a
 // value is the sum of three bf16 parts, whose exact products with the bf16 weights are summed in fp32.
@@ -31,7 +31,7 @@ constexpr int kFewThreads = 512, kFewWaves = kFewThreads / kWave;
 constexpr int kFewRowsTile = 16;
 // Weights of more than this in one launch, which the last-level cache does not hold until the next call anyway, are loaded past
 // it: packed, d = 4096, h = 16384, 20 experts 1 003 -> 917 us; below, a loop over one layer finds them there (d = 1024, h = 4096,
-// one expert 12.9 -> 14.6).  Row-major ones if their rows are whole lines of memory (few_dot_rows).
+// one expert 12.9 -> 14.6).  Row-major ones if their rows are whole lines of memory.
 constexpr long long kFewStreamBytes = 100ll << 20;
 
 // The routing as the second kernel reads it (front of the workspace; H follows at kFewHOffset)
@@ -182,35 +182,34 @@ __device__ __forceinline__ void few_groups(const int32_t* s_eid, int T, int C, F
   }
 }
 
-// k-steps in flight: what 128 registers hold beside the sums (x 16-byte loads of the tokens' operand a step).  16 waves of a compute
-// unit have 128 KiB of weights in flight with 8, which is enough: with the tokens' rows in LDS and 16 steps of weights in flight
-// d = 4096, h = 16384, 24 experts take 929 us instead of 902 (8 steps: 897), with loads kept in flight across the products 906,
-// with pairs of tiles that share the tokens' operand 931.
-constexpr int few_depth(int x) { return x <= 1 ? 8 : x <= 3 ? 4 : x <= 6 ? 2 : 1; }
+// k-steps of weights in flight, and products whose tokens' operands (XL 16-byte loads each) are, of the NB column tiles of these
+// steps: what 128 registers hold beside the sums.  16 waves of a compute unit have 128 KiB of weights in flight with 8 steps, which
+// is enough: d = 4096, h = 16384, 24 experts took 902 us with the tokens' operands of all steps in flight too, 929 with these in LDS
+// and 16 steps of weights (8 steps: 897), 906 with loads kept in flight across the products, 931 with pairs of tiles that share
+// the operands.  For more than one column tile the operands come in behind the products they are for: 64 tokens on 4 experts,
+// d = 2048, h = 8192, packed, 104 us with 2 steps of weights and all their operands in flight, 97 with 8 steps and 4 operands (8: 97).
+constexpr int few_depth(int XL) { return XL == 1 ? 8 : 4; }
+constexpr int few_ahead(int XL, int NB) { return NB == 1 ? few_depth(XL) : 5 - XL; }
 
-// A k-step's products: weights w, tokens' operand x as loaded
-template <bool X_F32, int NP, int NB>
-__device__ __forceinline__ void few_mul(f32x4 (&acc)[NB], const u32x4& w, const u32x4 (&x)[NB][X_F32 ? 2 : NP]) {
+// A k-step's products of a column tile: weights w, tokens' operand x as loaded
+template <bool X_F32, int NP>
+__device__ __forceinline__ void few_mul(f32x4& acc, const u32x4& w, const u32x4 (&x)[X_F32 ? 2 : NP]) {
+  u32x4 part[NP];
+  if constexpr (X_F32) {
 #pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    u32x4 part[NP];
-    if constexpr (X_F32) {
+    for (int i = 0; i < 4; ++i) {
+      uint32_t v[3];
+      split3(__uint_as_float(x[i / 2][2 * i % 4]), __uint_as_float(x[i / 2][2 * i % 4 + 1]), v);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t v[3];
-        split3(__uint_as_float(x[b][i / 2][2 * i % 4]), __uint_as_float(x[b][i / 2][2 * i % 4 + 1]), v);
-#pragma unroll
-        for (int p = 0; p < NP; ++p) part[p][i] = v[p];
-      }
-    } else {
-#pragma unroll
-      for (int p = 0; p < NP; ++p) part[p] = x[b][p];
+      for (int p = 0; p < NP; ++p) part[p][i] = v[p];
     }
+  } else {
 #pragma unroll
-    for (int p = 0; p < NP; ++p)
-      acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, part[p]),
-                                                       acc[b], 0, 0, 0);
+    for (int p = 0; p < NP; ++p) part[p] = x[p];
   }
+#pragma unroll
+  for (int p = 0; p < NP; ++p)
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, part[p]), acc, 0, 0, 0);
 }
 
 // A wave's share of a GEMM: steps s0 .. s1 - 1 of K for one 16-row tile of weights and NB column tiles of 16 tokens.  W: the
@@ -220,19 +219,27 @@ __device__ __forceinline__ void few_mul(f32x4 (&acc)[NB], const u32x4& w, const 
 // SEG = 2, 4: a tile is 16 / SEG rows, each SEG times side by side in the MFMA's rows with a SEG-th of K each, and so are up to
 // 16 / SEG tokens in its columns: SEG blocks on the diagonal of the result, which the caller adds, for a tile whose products
 // the rows of SEG times as many work-groups share.
+//
+// Row-major weights past the caches go by whole lines, two steps (64 k) at a time, which s0, s1 then count: a load takes the line of 8
+// rows (half lines are fetched twice), the first 8 lanes of a 16-lane row its first half and the others its second, and two
+// loads (rows 0 to 7 and 8 to 15) make two steps' operands by exchanging halves.  d = 4096, h = 16384, 20 experts: 1 049 us with
+// half lines through the caches, 929 so, 923 with the tiles out of step (one expert: 69, 66 and 51).
 template <bool PACKED, bool X_F32, int NP, int NB, int SEG, bool STREAM>
 __device__ __forceinline__ void few_dot(f32x4 (&acc)[NB], const char* __restrict__ W, const void* __restrict__ X,
                                         size_t plane, const int32_t* tok, int n, int tile, int Kdim, int Ndim, int s0,
                                         int s1) {
+  constexpr bool LINES = STREAM && !PACKED;
   constexpr int XL = X_F32 ? 2 : NP;  // 16-byte loads of a column tile and step
-  constexpr int D = few_depth(NB * XL);
+  constexpr int H = LINES ? 2 : 1, D = few_depth(XL) / H, A = few_ahead(XL, NB), ALL = D * H * NB;
   const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
-  constexpr int kStep = PACKED ? 16384 : 64, kXStep = X_F32 ? 128 : 64;
+  constexpr int kStep = PACKED ? 16384 : 64 * H, kXStep = X_F32 ? 128 : 64;
   constexpr int R = kFewRowsTile / SEG;
-  const int row = min(tile * R + l16 % R, Ndim - 1);  // (rows past the last repeat it: not stored)
-  const int seg = l16 / R, k_seg = Kdim / SEG;
+  // (rows past the last repeat it: not stored)
+  const int row = min(tile * R + (LINES ? l16 & 7 : l16 % R), Ndim - 1), row1 = min(tile * R + 8 + (l16 & 7), Ndim - 1);
+  const int seg = l16 / R, k_seg = Kdim / SEG, chunk = LINES ? q + 4 * (l16 >> 3) : q;
   const char* pw = PACKED ? W + (size_t)(row >> 8) * Kdim * 512 + (row & 255) * 64 + ((q ^ ((row >> 1) & 3)) << 4)
-                          : W + (size_t)row * Kdim * 2 + q * 16;
+                          : W + (size_t)row * Kdim * 2 + chunk * 16;
+  const char* pw1 = W + (size_t)row1 * Kdim * 2 + chunk * 16;  // (LINES)
   pw += (size_t)(seg * (k_seg / 32)) * kStep;
   const char* px[NB];
 #pragma unroll
@@ -240,131 +247,86 @@ __device__ __forceinline__ void few_dot(f32x4 (&acc)[NB], const char* __restrict
     px[b] = (const char*)X + ((size_t)tok[min(16 * b + l16 % R, n - 1)] * Kdim + seg * k_seg + q * 8) * (X_F32 ? 4 : 2);
 #pragma unroll
   for (int b = 0; b < NB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  u32x4 w[D], x[D][NB][XL];
-  auto load = [&](int u, int s) {
+  u32x4 w[D][H], x[A][XL];
+  auto load_w = [&](int u, int s) {
     const u32x4* p = (const u32x4*)(pw + (size_t)s * kStep);
-    w[u] = STREAM ? __builtin_nontemporal_load(p) : *p;
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int p = 0; p < XL; ++p)
-        x[u][b][p] = *(const u32x4*)(px[b] + (size_t)s * kXStep + (X_F32 ? p * 16 : p * plane * 2));
+    w[u][0] = STREAM ? __builtin_nontemporal_load(p) : *p;
+    if constexpr (LINES) w[u][1] = __builtin_nontemporal_load((const u32x4*)(pw1 + (size_t)s * kStep));
   };
-  auto mul = [&](int u) { few_mul<X_F32, NP, NB>(acc, w[u], x[u]); };
-  // Whole turns of D steps, in a cycle that begins at a place of its own in each of 16 neighbouring blocks of packed rows: in
-  // step, all waves read at multiples of a power of two, which are few of the memory's channels (d = 4096, h = 16384, 20
+  auto load_x = [&](int at, int s, int b) {
+#pragma unroll
+    for (int p = 0; p < XL; ++p) x[at][p] = *(const u32x4*)(px[b] + (size_t)s * kXStep + (X_F32 ? p * 16 : p * plane * 2));
+  };
+  // D steps (or lines) from s on, or fewer: all weights' loads and the first A products' tokens, then the products, the tokens of
+  // later ones behind them.  (Tokens behind their step's weights: d = 1600, h = 6400, five experts 46.0 us, behind all weights 47.5.)
+  auto turn = [&](int s, auto whole, int count) {
+    constexpr bool WHOLE = decltype(whole)::value;
+#pragma unroll
+    for (int u = 0; u < D; ++u)
+      if (WHOLE || u < count) {
+        load_w(u, s + u);
+#pragma unroll
+        for (int i = u * H * NB; i < (u + 1) * H * NB && i < A; ++i) load_x(i, s * H + i / NB, i % NB);
+      }
+#pragma unroll
+    for (int i = 0; i < ALL; ++i) {
+      const int u = i / (H * NB);
+      if (WHOLE || u < count) {
+        if constexpr (LINES) {
+          if (i % (H * NB) == 0) {  // lanes 8 to 15 of a row take the other lanes' second load, lanes 0 to 7 their first
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t lo = w[u][0][k], hi = w[u][1][k];
+              w[u][0][k] = __builtin_amdgcn_update_dpp(lo, hi, kDppRor8, 0xF, 0xC, false);
+              w[u][1][k] = __builtin_amdgcn_update_dpp(hi, lo, kDppRor8, 0xF, 0x3, false);
+            }
+          }
+        }
+        few_mul<X_F32, NP>(acc[i % NB], w[u][i / NB % H], x[i % A]);
+      }
+      const int next = i + A;
+      if (next < ALL && (WHOLE || next / (H * NB) < count)) load_x(i % A, s * H + next / NB, next % NB);
+    }
+  };
+  // Whole turns in a cycle that begins at a place of its own in neighbouring blocks of packed rows (tiles of row-major lines): in
+  // step, all waves read at multiples of a power of two, which are few of the memory's channels (packed, d = 4096, h = 16384, 20
   // experts: 952 -> 890 us).
-  const int full = min(s1, k_seg / 32), turns = max(full - s0, 0) / D;
-  int at = s0 + (PACKED ? (tile >> 4) & 15 : 0) * (turns >> 4) * D;
+  const int full = LINES ? s1 : min(s1, k_seg / 32), turns = max(full - s0, 0) / D;
+  int at = s0 + (PACKED ? ((tile >> 4) & 15) * (turns >> 4) : LINES ? (tile & 7) * (turns >> 3) : 0) * D;
   for (int i = 0; i < turns; ++i) {
-#pragma unroll
-    for (int u = 0; u < D; ++u) load(u, at + u);
-#pragma unroll
-    for (int u = 0; u < D; ++u) mul(u);
+    turn(at, std::true_type{}, D);
     at += D;
     if (at == s0 + turns * D) at = s0;
   }
   int s = s0 + turns * D;
-  // fewer than D steps are left: all their loads, then all their products
+  if (s < full) turn(s, std::false_type{}, full - s);
+  if constexpr (!LINES) {
+    s = max(s, full);
+    if (s < s1) {  // the step that ends behind K, where both operands are zeros past it
+      const bool in = s * 32 + q * 8 < k_seg;
+      w[0][0] = u32x4{0u, 0u, 0u, 0u};
+      if (in) load_w(0, s);
 #pragma unroll
-  for (int u = 0; u < D - 1; ++u)
-    if (s + u < full) load(u, s + u);
+      for (int b = 0; b < NB; ++b) {
 #pragma unroll
-  for (int u = 0; u < D - 1; ++u)
-    if (s + u < full) mul(u);
-  s = max(s, full);
-  if (s < s1) {  // the step that ends behind K, where both operands are zeros past it
-    const u32x4 zero = {0u, 0u, 0u, 0u};
-    w[0] = zero;
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int p = 0; p < XL; ++p) x[0][b][p] = zero;
-    if (s * 32 + q * 8 < k_seg) load(0, s);
-    mul(0);
-  }
-}
-
-// The same for row-major weights past the caches, two steps (128 bytes of a row, a line) at a time, [p0, p1): a load takes the whole
-// line of 8 rows (half lines are fetched twice), the first 8 lanes of a 16-lane row its first half and the others its second, and
-// two loads (rows 0 to 7 and 8 to 15) make two steps' operands by exchanging halves.  d = 4096, h = 16384, 20 experts: 1 049 us with
-// half lines through the caches, 929 so, 923 with the tiles out of step (one expert: 69, 66, 51).
-template <bool X_F32, int NP, int NB>
-__device__ __forceinline__ void few_dot_rows(f32x4 (&acc)[NB], const char* __restrict__ W, const void* __restrict__ X,
-                                             size_t plane, const int32_t* tok, int n, int tile, int Kdim, int Ndim, int p0,
-                                             int p1) {
-  constexpr int XL = X_F32 ? 2 : NP;
-  constexpr int D = (few_depth(NB * XL) + 1) / 2;
-  constexpr int XH = few_depth(NB * XL) > 1 ? 2 : 1;  // the second step's tokens too, or fetched after the first step's products
-  const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4, c = q + 4 * (l16 >> 3);
-  const int r0 = tile * kFewRowsTile + (l16 & 7);
-  const char* pw0 = W + (size_t)min(r0, Ndim - 1) * Kdim * 2 + c * 16;
-  const char* pw1 = W + (size_t)min(r0 + 8, Ndim - 1) * Kdim * 2 + c * 16;
-  const char* px[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b)
-    px[b] = (const char*)X + ((size_t)tok[min(16 * b + l16, n - 1)] * Kdim + q * 8) * (X_F32 ? 4 : 2);
-#pragma unroll
-  for (int b = 0; b < NB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  u32x4 w[D][2], x[D][XH][NB][XL];
-  auto load_w = [&](int u, int p) {
-    const u32x4 *a = (const u32x4*)(pw0 + (size_t)p * 128), *b = (const u32x4*)(pw1 + (size_t)p * 128);
-    w[u][0] = __builtin_nontemporal_load(a);
-    w[u][1] = __builtin_nontemporal_load(b);
-  };
-  auto load_x = [&](int u, int h, int p) {
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int i = 0; i < XL; ++i)
-        x[u][h % XH][b][i] = *(const u32x4*)(px[b] + (size_t)(2 * p + h) * (X_F32 ? 128 : 64) + (X_F32 ? i * 16 : i * plane * 2));
-  };
-  auto load = [&](int u, int p) {
-    load_w(u, p);
-#pragma unroll
-    for (int h = 0; h < XH; ++h) load_x(u, h, p);
-  };
-  auto mul = [&](int u, auto&& second) {
-    u32x4 a0, a1;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {  // lanes 8 to 15 of a row take the other lanes' second load, lanes 0 to 7 their first
-      a0[i] = __builtin_amdgcn_update_dpp(w[u][0][i], w[u][1][i], kDppRor8, 0xF, 0xC, false);
-      a1[i] = __builtin_amdgcn_update_dpp(w[u][1][i], w[u][0][i], kDppRor8, 0xF, 0x3, false);
+        for (int p = 0; p < XL; ++p) x[0][p] = u32x4{0u, 0u, 0u, 0u};
+        if (in) load_x(0, s, b);
+        few_mul<X_F32, NP>(acc[b], w[0][0], x[0]);
+      }
     }
-    few_mul<X_F32, NP, NB>(acc, a0, x[u][0]);
-    if constexpr (XH == 1) second();
-    few_mul<X_F32, NP, NB>(acc, a1, x[u][XH - 1]);
-  };
-  const int turns = (p1 - p0) / D;
-  int at = p0 + (tile & 7) * (turns >> 3) * D;  // (neighbouring tiles out of step, as in few_dot)
-  for (int i = 0; i < turns; ++i) {
-#pragma unroll
-    for (int u = 0; u < D; ++u) load(u, at + u);
-#pragma unroll
-    for (int u = 0; u < D; ++u) mul(u, [&] { load_x(u, 1, at + u); });
-    at += D;
-    if (at == p0 + turns * D) at = p0;
   }
-  int p = p0 + turns * D;
-#pragma unroll
-  for (int u = 0; u < D - 1; ++u)
-    if (p + u < p1) load(u, p + u);
-#pragma unroll
-  for (int u = 0; u < D - 1; ++u)
-    if (p + u < p1) mul(u, [&] { load_x(u, 1, p + u); });
 }
 
 // All tiles of all groups, over the grid's waves: epilogue(token, first row of weights, 4 sums).  MAXB: column tiles at most (of all
 // tokens).  per_wave: 1 / waves of the grid.  red: LDS for the sums of a tile's waves but the first.
 constexpr int few_red(int maxb) { return (kFewWaves - 1) * maxb * 64; }
-template <bool PACKED, bool X_F32, int NP, int MAXB, int SEG, class F>
+template <bool PACKED, bool X_F32, int NP, int MAXB, int SEG, bool STREAM, class F>
 __device__ __forceinline__ void few_gemm(const FewTable* t, const char* W, const void* X, size_t plane, int Kdim, int Ndim,
                                          float per_wave, float4* red, F&& epilogue) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   constexpr int R = kFewRowsTile / SEG;
   const unsigned tiles = (unsigned)(Ndim + R - 1) / R, items = t->groups * tiles;
   const int steps = (Kdim / SEG + 31) / 32;
-  const bool stream = (PACKED || (SEG == 1 && Kdim % 64 == 0)) && (long long)t->groups * Ndim * Kdim * 2 > kFewStreamBytes;
   // 2^lks waves per tile: the fewest k-steps one after another, counting four for a turn of tiles' latency
   int lks = 0;
   float least = 3e38f;
@@ -375,8 +337,8 @@ __device__ __forceinline__ void few_gemm(const FewTable* t, const char* W, const
     if (cost < least) { least = cost; lks = i; }
   }
   const int ks = 1 << lks, per = kFewWaves >> lks, sub = wave & (ks - 1), mine = wave >> lks;
-  const int lines = stream ? 2 : 1;  // (streamed row-major weights go by lines of two steps)
-  const int s0 = (steps / lines * sub >> lks) * lines, s1 = (steps / lines * (sub + 1) >> lks) * lines;
+  const int units = !PACKED && STREAM ? steps / 2 : steps;  // (row-major weights past the caches go by lines of two steps)
+  const int s0 = units * sub >> lks, s1 = units * (sub + 1) >> lks;
   int u = 0;
   unsigned at = blockIdx.x * per + mine;  // number in group u
   for (unsigned i0 = blockIdx.x * per; i0 < items; i0 += gridDim.x * per, at += gridDim.x * per) {
@@ -392,9 +354,7 @@ __device__ __forceinline__ void few_gemm(const FewTable* t, const char* W, const
     auto dot = [&](auto nb_) {
       constexpr int NB = decltype(nb_)::value;
       f32x4 part[NB];
-      if (!stream) few_dot<PACKED, X_F32, NP, NB, SEG, false>(part, We, X, plane, tok, n, tile, Kdim, Ndim, s0, s1);
-      else if constexpr (PACKED) few_dot<PACKED, X_F32, NP, NB, SEG, true>(part, We, X, plane, tok, n, tile, Kdim, Ndim, s0, s1);
-      else if constexpr (SEG == 1) few_dot_rows<X_F32, NP, NB>(part, We, X, plane, tok, n, tile, Kdim, Ndim, s0 / 2, s1 / 2);
+      few_dot<PACKED, X_F32, NP, NB, SEG, STREAM>(part, We, X, plane, tok, n, tile, Kdim, Ndim, s0, s1);
 #pragma unroll
       for (int b = 0; b < NB; ++b) acc[b] = part[b];
     };
@@ -444,7 +404,7 @@ __device__ __forceinline__ void few_gemm(const FewTable* t, const char* W, const
 
 // (four waves per SIMD: two work-groups per compute unit)
 
-template <bool BF16, bool PACKED, int MAXB, int SEG>
+template <bool BF16, bool PACKED, int MAXB, int SEG, bool STREAM>
 __global__ __launch_bounds__(kFewThreads, 4) void few_in_kernel(const void* __restrict__ x, const float* __restrict__ g,
                                                                 const float* __restrict__ eps,
                                                                 const char* __restrict__ W, int32_t* __restrict__ eid,
@@ -471,7 +431,7 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_in_kernel(const void* __re
   }
   constexpr int NP = BF16 ? 1 : 3;
   const size_t plane = (size_t)T * h;
-  few_gemm<PACKED, !BF16, NP, MAXB, SEG>(&t, W, x, 0, d, h, per_wave, red, [&](int m, int r, const f32x4& a) {
+  few_gemm<PACKED, !BF16, NP, MAXB, SEG, STREAM>(&t, W, x, 0, d, h, per_wave, red, [&](int m, int r, const f32x4& a) {
     uint16_t* dst = H + (size_t)m * h + r;
     if constexpr (BF16) {
       *(uint2*)dst = make_uint2(pack_bf16x2(gelu_bf16(a[0]), gelu_bf16(a[1])), pack_bf16x2(gelu_bf16(a[2]), gelu_bf16(a[3])));
@@ -485,7 +445,7 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_in_kernel(const void* __re
   });
 }
 
-template <bool BF16, bool PACKED, int MAXB, int SEG>
+template <bool BF16, bool PACKED, int MAXB, int SEG, bool STREAM>
 __global__ __launch_bounds__(kFewThreads, 4) void few_out_kernel(const uint16_t* __restrict__ H,
                                                                  const FewTable* __restrict__ table,
                                                                  const int32_t* __restrict__ slot,
@@ -502,7 +462,7 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_out_kernel(const uint16_t*
       if (slot[m] < 0)
         for (int c = threadIdx.x; c < chunks; c += kFewThreads) ((uint4*)y)[(size_t)m * chunks + c] = make_uint4(0, 0, 0, 0);
   }
-  few_gemm<PACKED, false, BF16 ? 1 : 3, MAXB, SEG>(&t, W, H, (size_t)T * h, h, d, per_wave, red, [&](int m, int r, const f32x4& a) {
+  few_gemm<PACKED, false, BF16 ? 1 : 3, MAXB, SEG, STREAM>(&t, W, H, (size_t)T * h, h, d, per_wave, red, [&](int m, int r, const f32x4& a) {
     const float f = weighted ? w[m] : 1.0f;
     if constexpr (BF16)
       *(uint2*)((uint16_t*)y + (size_t)m * d + r) = make_uint2(pack_bf16x2(f * a[0], f * a[1]), pack_bf16x2(f * a[2], f * a[3]));
@@ -547,6 +507,10 @@ extern "C" int locmoe_layer_few(const locmoe_desc* desc, const void* x, const fl
       seg *= 2;
     return seg;
   };
+  // past the caches? (groups: as many as there can be)
+  auto streams = [&](int N, int K, int seg) {
+    return seg == 1 && (desc->w_packed || K % 64 == 0) && (long long)std::min(T, E) * N * K * 2 > kFewStreamBytes;
+  };
   // two work-groups per compute unit, no more than there can be tiles (of up to eight waves each)
   auto groups = [&](int N, int seg) {
     return (unsigned)std::min<long long>(2 * cu_count(), (long long)std::min(T, E) * ceil_div(N, kFewRowsTile / seg));
@@ -556,11 +520,11 @@ extern "C" int locmoe_layer_few(const locmoe_desc* desc, const void* x, const fl
     constexpr int MAXB = decltype(maxb)::value;
     const int seg_in = segments(h, d), seg_out = segments(d, h);
     const unsigned in = groups(h, seg_in), out = groups(d, seg_out);
-    auto k_in = few_in_kernel<BF, PK, MAXB, 1>;
-    auto k_out = few_out_kernel<BF, PK, MAXB, 1>;
+    auto k_in = streams(h, d, seg_in) ? few_in_kernel<BF, PK, MAXB, 1, true> : few_in_kernel<BF, PK, MAXB, 1, false>;
+    auto k_out = streams(d, h, seg_out) ? few_out_kernel<BF, PK, MAXB, 1, true> : few_out_kernel<BF, PK, MAXB, 1, false>;
     if constexpr (MAXB == 1) {
-      if (seg_in > 1) k_in = seg_in == 2 ? few_in_kernel<BF, PK, 1, 2> : few_in_kernel<BF, PK, 1, 4>;
-      if (seg_out > 1) k_out = seg_out == 2 ? few_out_kernel<BF, PK, 1, 2> : few_out_kernel<BF, PK, 1, 4>;
+      if (seg_in > 1) k_in = seg_in == 2 ? few_in_kernel<BF, PK, 1, 2, false> : few_in_kernel<BF, PK, 1, 4, false>;
+      if (seg_out > 1) k_out = seg_out == 2 ? few_out_kernel<BF, PK, 1, 2, false> : few_out_kernel<BF, PK, 1, 4, false>;
     }
     hipLaunchKernelGGL(k_in, dim3(in), dim3(kFewThreads), 0, s, x, g, eps, (const char*)W_in, eid, w, slot, table, H, T, d, E, h,
                        desc->C, desc->relu, plan, 1.0f / (float)(in * kFewWaves));

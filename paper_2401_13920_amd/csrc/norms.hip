@@ -4,7 +4,10 @@
 //   locmoe_combine_norm_bwd   its gradients: dout, dw, dgamma
 //   locmoe_dispatch_norm_bwd  dxn = dsend[slot] + (E/d) dg, and the norm's backward: dx, dgamma
 // Every row is read once, held in registers between the sum over it and its use, and written once.  LPR lanes share a row,
-// CPL 16-byte chunks each.  All of it is bound by memory.
+// CPL 16-byte chunks each.  All of it is bound by memory, loaded and stored past the caches: with T = 65 536 tokens, d = 4096, E = 64,
+// bf16, 31 200 of them kept, norm_gate takes 196 us (1.09 GB, 5.6 TB/s), combine_norm 217 (1.34 GB, 6.2), combine_norm_bwd 158
+// (0.79 GB, 5.0) and dispatch_norm_bwd 323 (1.90 GB, 5.9); a plain copy reaches 5.7.  With 64 tokens of d = 1024 each takes 3.4 us,
+// less than its launch from the host.
 //
 // A column's gradient (dgamma) is a sum over tokens: a work-group sums its rows in registers, writes one row of partial
 // sums to the workspace, and a second kernel adds those in a fixed order: no atomics, the same bits every time.
@@ -249,6 +252,10 @@ __device__ __forceinline__ void store_partial(const float (&acc)[CPL][V], float*
   }
 }
 
+// A work-group walks the tokens a stride apart, with the next one's slot in flight; dropped tokens cost that slot alone.  Gathered
+// rows, a barrier a row (of more than a wave) and the sums in registers leave 5.0 TB/s; half as many work-groups or twice as many
+// take 4 to 11 % longer (both gradients together 497 us, 512 of them 555, 2 048 506), the next row's loads ahead of this one's
+// sum 565.
 // With n the row that the forward multiplied (out r, or out without the norm) and u = scale gamma dy:
 //   dw = <u, n>,   dgamma += scale w dy n,   dout = r w (u - n dw / d), or w u without the norm.
 template <bool BF16, int LPR, int CPL, bool POST>
@@ -392,8 +399,8 @@ __global__ __launch_bounds__(threads_of<LPR>()) void dispatch_norm_bwd_kernel(
 }
 
 // dgamma[j] = sum of column j over the rows of partial sums.  A work-group makes 16 columns: four lanes of four columns, 64 row
-// groups with up to 16 loads in flight each, whose sums are added in a fixed order through LDS.  (64 columns per work-group leave
-// most compute units idle: 1 024 rows of 4 096 columns 8.4 us.)
+// groups with up to 16 loads in flight each, whose sums are added in a fixed order through LDS.  1 024 rows of 4 096 columns: 7.0 us
+// (64 columns per work-group, which leave most compute units idle, 8.4), of 1 600 columns 4.7.
 constexpr int kSumCols = 16;
 __global__ __launch_bounds__(256) void column_sum_kernel(const float* __restrict__ part, float* __restrict__ dgamma,
                                                          int rows, int d) {

@@ -400,8 +400,9 @@ int locmoe_dispatch_norm_bwd(const locmoe_desc* desc, const void* dsend, const i
  *   bf16.  The order of the sums depends on T and the routing, so bits may differ from the other path's, and a token's with
  *   the batch it is in; the same call gives the same bits.
  *   x device [T,d] of x_dtype; g device [T,E] fp32 (gating values from locmoe_norm_gate or locmoe_gate_dense) or NULL (formed
- *   here as locmoe_gate does, up to the order of the additions); eps device [E] fp32 or NULL; W_in, W_out row-major or packed
- *   as desc->w_packed says; eid, slot device [T] i32, w device [T] fp32, y device [T,d] of x_dtype (may be x itself);
+ *   here as locmoe_gate does, up to the order of the additions); eps device [E] fp32 or NULL (with relu = 0 a value of -inf masks
+ *   an expert: no token takes it, and it has no part in a score; a token without any other has eid 0 and w NaN); W_in, W_out
+ *   row-major or packed as desc->w_packed says; eid, slot device [T] i32, w device [T] fp32, y device [T,d] of x_dtype (may be x itself);
  *   ws device scratch of >= locmoe_layer_few_workspace_bytes (0: an invalid descriptor, or too many tokens), nothing in it
  *   has to be set.  desc->N, alpha and mu are not used.  LOCMOE_ERR_SHAPE if T > LOCMOE_FEW_MAX_TOKENS
  *   or d or h > LOCMOE_FEW_MAX_WIDTH. */

@@ -172,6 +172,25 @@ def test_masked_experts(env, E):
             assert (L.eid % 2 == 1).all() and torch.isfinite(L.w).all()
 
 
+@pytest.mark.parametrize("E", [1, 4, 96])
+def test_token_without_experts(env, E):
+    """Every expert masked: expert 0 and a score of NaN, which stay with that token."""
+    torch, lm = env
+    for T in (1, 5, 40):
+        print(f"[few none] E={E} T={T}", flush=True)
+        L = Layer(env, T, 96, E, 16, T, relu=False)
+        g = L.rng.standard_normal((T, E)).astype(np.float32)
+        L.call(torch.from_numpy(g).cuda())
+        eid, y = L.eid.clone(), L.y.clone()
+        g[T // 2] = -np.inf
+        L.call(torch.from_numpy(g).cuda())
+        others = [m for m in range(T) if m != T // 2]
+        assert L.eid[T // 2] == 0 and torch.isnan(L.w[T // 2]) and torch.isnan(L.y[T // 2]).all()
+        assert torch.equal(L.eid[others], eid[others]) and torch.isfinite(L.y[others]).all()
+        if E == 1:     # (elsewhere another group's size may change how a GEMM is cut)
+            assert torch.equal(L.y[others], y[others])
+
+
 def test_all_tokens_alike(env):
     """The same token 64 times: one group of 64, of which the capacity keeps the first ones."""
     torch, lm = env

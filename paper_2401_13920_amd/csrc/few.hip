@@ -42,6 +42,9 @@ struct FewTable {
   int32_t token[kFewTokens];
 };
 constexpr size_t kFewHOffset = 1024;
+// Values from row to row of H: where rows would be whole lines, half a line more, so that the 64 bytes that a load takes of each of 16
+// rows are not all first or all second halves (64 tokens on one expert, d = 2048, h = 8192: 73 -> 67 us; a whole line more: nothing)
+__host__ __device__ constexpr int few_h_row(int h) { return h % 64 == 0 ? h + 32 : h; }
 static_assert(sizeof(FewTable) <= kFewHOffset, "");
 
 // Two fp32 values -> three bf16 parts of each (bits 0..7, 8..15 and 16..23 of the significand: cut, so that every remainder is
@@ -187,9 +190,9 @@ __device__ __forceinline__ void few_groups(const int32_t* s_eid, int T, int C, F
 // is enough: d = 4096, h = 16384, 24 experts took 902 us with the tokens' operands of all steps in flight too, 929 with these in LDS
 // and 16 steps of weights (8 steps: 897), 906 with loads kept in flight across the products, 931 with pairs of tiles that share
 // the operands.  For more than one column tile the operands come in behind the products they are for: 64 tokens on 4 experts,
-// d = 2048, h = 8192, packed, 104 us with 2 steps of weights and all their operands in flight, 97 with 8 steps and 4 operands (8: 97).
+// d = 2048, h = 8192, packed, 104 us with 2 steps of weights and all their operands in flight, 96 so.
 constexpr int few_depth(int XL) { return XL == 1 ? 8 : 4; }
-constexpr int few_ahead(int XL, int NB) { return NB == 1 ? few_depth(XL) : 5 - XL; }
+constexpr int few_ahead(int XL, int NB) { return NB == 1 ? few_depth(XL) : (NB == 2 ? 2 : 1) * (5 - XL); }
 
 // A k-step's products of a column tile: weights w, tokens' operand x as loaded
 template <bool X_F32, int NP>
@@ -213,8 +216,8 @@ __device__ __forceinline__ void few_mul(f32x4& acc, const u32x4& w, const u32x4 
 }
 
 // A wave's share of a GEMM: steps s0 .. s1 - 1 of K for one 16-row tile of weights and NB column tiles of 16 tokens.  W: the
-// expert's weights.  Operand B is the tokens' rows: bf16 (NP planes `plane` elements apart) or, with X_F32, fp32.  STREAM: the
-// weights are loaded past the caches.
+// expert's weights.  Operand B is the tokens' rows, x_row values apart: bf16 (NP planes `plane` elements apart) or, with X_F32, fp32.
+// STREAM: the weights are loaded past the caches.
 //
 // SEG = 2, 4: a tile is 16 / SEG rows, each SEG times side by side in the MFMA's rows with a SEG-th of K each, and so are up to
 // 16 / SEG tokens in its columns: SEG blocks on the diagonal of the result, which the caller adds, for a tile whose products
@@ -226,7 +229,7 @@ __device__ __forceinline__ void few_mul(f32x4& acc, const u32x4& w, const u32x4 
 // half lines through the caches, 929 so, 923 with the tiles out of step (one expert: 69, 66 and 51).
 template <bool PACKED, bool X_F32, int NP, int NB, int SEG, bool STREAM>
 __device__ __forceinline__ void few_dot(f32x4 (&acc)[NB], const char* __restrict__ W, const void* __restrict__ X,
-                                        size_t plane, const int32_t* tok, int n, int tile, int Kdim, int Ndim, int s0,
+                                        size_t plane, int x_row, const int32_t* tok, int n, int tile, int Kdim, int Ndim, int s0,
                                         int s1) {
   constexpr bool LINES = STREAM && !PACKED;
   constexpr int XL = X_F32 ? 2 : NP;  // 16-byte loads of a column tile and step
@@ -244,7 +247,7 @@ __device__ __forceinline__ void few_dot(f32x4 (&acc)[NB], const char* __restrict
   const char* px[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b)  // columns past the group's tokens repeat the last one (not stored)
-    px[b] = (const char*)X + ((size_t)tok[min(16 * b + l16 % R, n - 1)] * Kdim + seg * k_seg + q * 8) * (X_F32 ? 4 : 2);
+    px[b] = (const char*)X + ((size_t)tok[min(16 * b + l16 % R, n - 1)] * x_row + seg * k_seg + q * 8) * (X_F32 ? 4 : 2);
 #pragma unroll
   for (int b = 0; b < NB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
   u32x4 w[D][H], x[A][XL];
@@ -321,7 +324,7 @@ __device__ __forceinline__ void few_dot(f32x4 (&acc)[NB], const char* __restrict
 // tokens).  per_wave: 1 / waves of the grid.  red: LDS for the sums of a tile's waves but the first.
 constexpr int few_red(int maxb) { return (kFewWaves - 1) * maxb * 64; }
 template <bool PACKED, bool X_F32, int NP, int MAXB, int SEG, bool STREAM, class F>
-__device__ __forceinline__ void few_gemm(const FewTable* t, const char* W, const void* X, size_t plane, int Kdim, int Ndim,
+__device__ __forceinline__ void few_gemm(const FewTable* t, const char* W, const void* X, size_t plane, int x_row, int Kdim, int Ndim,
                                          float per_wave, float4* red, F&& epilogue) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   constexpr int R = kFewRowsTile / SEG;
@@ -354,7 +357,7 @@ __device__ __forceinline__ void few_gemm(const FewTable* t, const char* W, const
     auto dot = [&](auto nb_) {
       constexpr int NB = decltype(nb_)::value;
       f32x4 part[NB];
-      few_dot<PACKED, X_F32, NP, NB, SEG, STREAM>(part, We, X, plane, tok, n, tile, Kdim, Ndim, s0, s1);
+      few_dot<PACKED, X_F32, NP, NB, SEG, STREAM>(part, We, X, plane, x_row, tok, n, tile, Kdim, Ndim, s0, s1);
 #pragma unroll
       for (int b = 0; b < NB; ++b) acc[b] = part[b];
     };
@@ -395,7 +398,8 @@ __device__ __forceinline__ void few_gemm(const FewTable* t, const char* W, const
 #pragma unroll
       for (int b = 0; b < MAXB; ++b) {
         const int c = 16 * b + (lane & 15), r = tile * R + (lane >> 4) * 4;
-        if (c < n && (SEG == 1 || (lane < 64 / SEG && (lane & 15) < R)) && r < Ndim) epilogue(tok[c], r, acc[b]);  // (Ndim is a multiple of 8: the quad is inside or outside)
+        // (Ndim is a multiple of 8: the quad is inside or outside)
+        if (c < n && (SEG == 1 || (lane < 64 / SEG && (lane & 15) < R)) && r < Ndim) epilogue(tok[c], r, acc[b]);
       }
     }
     if (ks > 1 && i0 + gridDim.x * per < items) __syncthreads();  // (red has been read)
@@ -403,7 +407,6 @@ __device__ __forceinline__ void few_gemm(const FewTable* t, const char* W, const
 }
 
 // (four waves per SIMD: two work-groups per compute unit)
-
 template <bool BF16, bool PACKED, int MAXB, int SEG, bool STREAM>
 __global__ __launch_bounds__(kFewThreads, 4) void few_in_kernel(const void* __restrict__ x, const float* __restrict__ g,
                                                                 const float* __restrict__ eps,
@@ -430,9 +433,9 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_in_kernel(const void* __re
     for (int i = threadIdx.x; i < (int)(sizeof(FewTable) / 4); i += kFewThreads) ((int32_t*)table)[i] = ((int32_t*)&t)[i];
   }
   constexpr int NP = BF16 ? 1 : 3;
-  const size_t plane = (size_t)T * h;
-  few_gemm<PACKED, !BF16, NP, MAXB, SEG, STREAM>(&t, W, x, 0, d, h, per_wave, red, [&](int m, int r, const f32x4& a) {
-    uint16_t* dst = H + (size_t)m * h + r;
+  const size_t plane = (size_t)T * few_h_row(h);
+  few_gemm<PACKED, !BF16, NP, MAXB, SEG, STREAM>(&t, W, x, 0, d, d, h, per_wave, red, [&](int m, int r, const f32x4& a) {
+    uint16_t* dst = H + (size_t)m * few_h_row(h) + r;
     if constexpr (BF16) {
       *(uint2*)dst = make_uint2(pack_bf16x2(gelu_bf16(a[0]), gelu_bf16(a[1])), pack_bf16x2(gelu_bf16(a[2]), gelu_bf16(a[3])));
     } else {
@@ -462,7 +465,7 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_out_kernel(const uint16_t*
       if (slot[m] < 0)
         for (int c = threadIdx.x; c < chunks; c += kFewThreads) ((uint4*)y)[(size_t)m * chunks + c] = make_uint4(0, 0, 0, 0);
   }
-  few_gemm<PACKED, false, BF16 ? 1 : 3, MAXB, SEG, STREAM>(&t, W, H, (size_t)T * h, h, d, per_wave, red, [&](int m, int r, const f32x4& a) {
+  few_gemm<PACKED, false, BF16 ? 1 : 3, MAXB, SEG, STREAM>(&t, W, H, (size_t)T * few_h_row(h), few_h_row(h), h, d, per_wave, red, [&](int m, int r, const f32x4& a) {
     const float f = weighted ? w[m] : 1.0f;
     if constexpr (BF16)
       *(uint2*)((uint16_t*)y + (size_t)m * d + r) = make_uint2(pack_bf16x2(f * a[0], f * a[1]), pack_bf16x2(f * a[2], f * a[3]));
@@ -478,7 +481,7 @@ extern "C" size_t locmoe_layer_few_workspace_bytes(const locmoe_desc* desc) {
   using namespace locmoe;
   if (check_desc(desc) != LOCMOE_OK || desc->T > kFewTokens || std::max(desc->d, desc->h) > LOCMOE_FEW_MAX_WIDTH) return 0;
   const size_t planes = desc->x_dtype == LOCMOE_BF16 ? 1 : 3;
-  return (kFewHOffset + planes * (size_t)desc->T * (size_t)desc->h * 2 + 255) & ~(size_t)255;
+  return (kFewHOffset + planes * (size_t)desc->T * (size_t)few_h_row(desc->h) * 2 + 255) & ~(size_t)255;
 }
 
 extern "C" int locmoe_layer_few(const locmoe_desc* desc, const void* x, const float* g, const float* eps, const void* W_in,

@@ -96,6 +96,9 @@ int locmoe_gate(const locmoe_desc* desc, const void* x, float* g, void* stream);
  *   D_l[i] = (#tokens whose home is node(i)) / (T * #experts on node(i)): every token spread
  *   evenly over the experts of its home node.  0 ln 0 = 0; KL = +inf if D_l[i] = 0 < D_c[i].
  *   home NULL: stats[1..4] = 0.
+ *   With relu = 0 a value of -inf masks an expert: no token takes it, and it has no part in a score.  A NaN is never the
+ *   largest (with relu = 1 it counts as 0).  A token for which that leaves no expert has eid 0; its w is NaN, as is that of
+ *   a token with a NaN or +inf among its values G, and what it adds to Psum and the sums of stats.
  *   g device [T,E] fp32; eps device [E] fp32 or NULL; home device [T] i32 in [0,N) or NULL;
  *   e2n device [E] i32 in [0,N) or NULL (= e / (E/N), which then needs E % N == 0);
  *   eid device [T] i32, w device [T] fp32, cnt device [E] i32, Psum device [E] fp32,

@@ -111,6 +111,9 @@ __device__ __forceinline__ void route_tokens(const float* __restrict__ g, const 
         if (x > best) { best = x; bi = i; }    // strict: lowest index wins ties
       }
       group_argmax<S>(best, bi);
+      // (nothing above -inf: every expert masked, or every value a NaN.  The index stays one, whoever counts or gathers with it;
+      // that there was no choice shows in w, which is NaN.)
+      bi = bi < E ? bi : 0;
       float z[EPL], zs = 0.f;
 #pragma unroll
       for (int k = 0; k < EPL; ++k) {

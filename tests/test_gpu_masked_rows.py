@@ -1,0 +1,128 @@
+"""Tokens that a mask or a NaN leaves without an expert, through locmoe_route and the block's steps behind it: every index stays
+one of an expert, and other tokens keep their results.
+
+A score is 1 / sum exp(v - best): the argument's rounding is at most |v - best| f, 8 f here, the exponential's 2 f, the sum's
+E f and the quotient's 2 f, f = 2^-24: (E + 12) f.
+"""
+import numpy as np
+import pytest
+
+from test_gpu_block import Setup
+from paper_2401_13920_amd import workloads as wl
+
+pytestmark = pytest.mark.gpu
+
+F = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+    from paper_2401_13920_amd import harness, locmoe as lm
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    lm.lib()
+    return torch, lm, harness
+
+
+def expected(G, relu):
+    """eid and w (NaN where there is no choice or a NaN takes part) of values G, float32."""
+    if relu:
+        G = np.where(np.isnan(G), 0.0, np.maximum(G, 0.0)).astype(np.float32)
+    eid = np.argmax(np.where(np.isnan(G), -np.inf, G), axis=1)
+    G = G.astype(np.float64)
+    with np.errstate(invalid="ignore"):
+        return eid, 1.0 / np.exp(G - G[np.arange(len(G)), eid][:, None]).sum(axis=1)
+
+
+def rows(rng, T, E):
+    """Gating values in [-4, 4] among which some tokens have nothing, a NaN, a mask over all but one or over the first half."""
+    g = rng.uniform(-4.0, 4.0, (T, E)).astype(np.float32)
+    g[0] = -np.inf
+    if T > 1:
+        g[T - 1] = np.nan
+    if T > 6:
+        g[2] = -np.inf
+        g[2, E - 1] = -3.0
+        g[3, :E // 2] = -np.inf
+        g[4, 0] = np.nan
+        g[5, E // 2:] = np.nan
+        g[T // 2] = np.where(np.arange(E) % 2, np.nan, -np.inf)
+    return g
+
+
+# one launch and two, one expert and several a lane, a work-group's tokens and more
+@pytest.mark.parametrize("T,E,N", [(1, 1, 1), (1, 4, 2), (9, 5, 5), (192, 16, 4), (2049, 4, 2), (700, 64, 8), (4099, 96, 6),
+                                   (300, 300, 3), (65, 1024, 16)])
+@pytest.mark.parametrize("relu", [False, True])
+def test_route(env, T, E, N, relu):
+    torch, lm, _ = env
+    print(f"[route masked] T={T} E={E} N={N} relu={relu}", flush=True)
+    rng = np.random.default_rng(T + E)
+    g = rows(rng, T, E)
+    desc = lm.make_desc(T, 8 * E, E, N, 8, T, relu=relu)
+    i32, f32 = dict(dtype=torch.int32, device="cuda"), dict(dtype=torch.float32, device="cuda")
+    home = torch.from_numpy(rng.integers(0, N, T).astype(np.int32)).cuda()
+    e2n = torch.from_numpy((np.arange(E) % N).astype(np.int32)).cuda()
+    n = lm.locmoe_workspace_bytes(desc)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    for eps in (None, np.full(E, -np.inf, np.float32)):
+        for map_ in (e2n, None):        # (None: node e / (E / N))
+            eid, w, cnt = torch.full((T,), 99, **i32), torch.full((T,), 7.0, **f32), torch.full((E,), 99, **i32)
+            Psum, stats = torch.empty(E, **f32), torch.empty(8, **f32)
+            e = None if eps is None else torch.from_numpy(eps).cuda()
+            lm.locmoe_route(desc, torch.from_numpy(g).cuda(), e, home, map_, eid, w, cnt, Psum, stats, ws, n)
+            want, score = expected(g if eps is None else g + eps, relu)
+            assert np.array_equal(eid.cpu().numpy(), want)
+            assert np.array_equal(cnt.cpu().numpy(), np.bincount(want, minlength=E))
+            got = w.double().cpu().numpy()
+            assert np.array_equal(np.isnan(got), np.isnan(score))
+            live = ~np.isnan(score)
+            assert (np.abs(got - score)[live] <= (E + 12) * F * score[live]).all()
+
+
+def clean_and_nan(env, T, dtype):
+    """A block whose gate has no ReLU, and the same with a NaN in a token of expert 0."""
+    torch, lm, _ = env
+    s = Setup(env, wl.small_config(T=T, d=192, E=6, N=3, h=104, dtype=dtype), T)
+    s.desc.relu, s.desc.mu = 0, 0.0
+    lm.forward_block(s.desc, s.xd, s.homed, None, *s.Wd, s.block, s.b, s.kb)
+    m = int((s.b.eid == 0).nonzero()[0, 0])
+    bad = s.xd.clone()
+    bad[m, 77] = float("nan")
+    return s, bad, m
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [40, 700])
+def test_block_with_a_nan_token(env, T, dtype):
+    """The norm makes all of the token NaN, its gating values too: expert 0, as before, and no other token changes."""
+    torch, lm, _ = env
+    print(f"[block NaN] T={T} {dtype}", flush=True)
+    s, bad, m = clean_and_nan(env, T, dtype)
+    gb, others = lm.alloc_grad_buffers(s.desc), [k for k in range(T) if k != m]
+    got = []
+    for x in (s.xd, bad):
+        lm.forward_block_train(s.desc, x, s.homed, None, *s.Wd, s.block, s.b, s.kb, gb)
+        lm.backward_block(s.desc, s.dyd, x, s.homed, None, *s.Wt, s.block, s.b, s.kb, gb)
+        got.append([t.clone() for t in (s.b.eid, s.b.slot, s.b.cnt, s.b.y[others], gb.dx[others], gb.dW_in[1:], gb.dW_out[1:])])
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert torch.isnan(s.b.w[m]) and torch.isnan(s.b.y[m]).all() and torch.isnan(gb.dx[m]).all()
+    assert all(torch.isfinite(t).all() for t in got[0][3:])
+    if T <= lm.LOCMOE_FEW_MAX_TOKENS:
+        lm.decode_block(s.desc, bad, *s.Wd, s.block, s.b, s.kb)
+        assert torch.equal(s.b.eid, got[0][0]) and torch.isnan(s.b.y[m]).all() and torch.isfinite(s.b.y[others]).all()
+
+
+def test_block_without_experts(env):
+    """Every expert masked: all tokens to expert 0 with a score of NaN; those past its capacity pass on the residual."""
+    torch, lm, hz = env
+    s = Setup(env, wl.small_config(T=50, d=192, E=6, N=3, h=104), 20)
+    s.desc.relu = 0
+    eps = torch.full((6,), -float("inf"), device="cuda")
+    for run in (lambda: lm.forward_block(s.desc, s.xd, s.homed, None, *s.Wd, s.block, s.b, s.kb, eps=eps),
+                lambda: lm.decode_block(s.desc, s.xd, *s.Wd, s.block, s.b, s.kb, eps=eps)):
+        s.b.y.fill_(7.0)
+        run()
+        assert (s.b.eid == 0).all() and torch.isnan(s.b.w).all()
+        assert (s.b.slot[:20] >= 0).all() and (s.b.slot[20:] == -1).all()
+        assert torch.isnan(s.b.y[:20]).all() and torch.equal(s.b.y[20:], s.xd[20:])

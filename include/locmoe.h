@@ -281,7 +281,8 @@ int locmoe_combine_bwd(const locmoe_desc* desc, const void* dy, const void* out,
 /* Eq. 3, the ReLU below it and the two batch losses, backward.  With s = g + eps, G = ReLU(s) (or s if
  * desc->relu == 0), p = softmax(G) recomputed as the forward did:
  *   coef[i] = alpha n f_i / T  (Eq. 5, f_i = cnt[i]/T fixed)  +  mu (ln(P_i / D_l[i]) + 1) / T  (Eq. 6 through
- *             P_i = Psum[i]/T; only if home != NULL and mu != 0; D_l as in locmoe_route);
+ *             P_i = Psum[i]/T; only if home != NULL and mu != 0, and not for P_i = 0, as of an expert masked by -inf;
+ *             D_l as in locmoe_route);
  *   dp[m,i] = [i = eid[m]] dw[m] + coef[i];   dG = p * (dp - <p, dp>);   dg[m,i] = dG[m,i] where s > 0 (ReLU).
  *   g device [T,E] fp32; eps device [E] or NULL; home device [T] or NULL; e2n device [E] or NULL (as in
  *   locmoe_route); eid device [T]; cnt device [E] i32 and Psum device [E] fp32 from locmoe_route; dw device [T];

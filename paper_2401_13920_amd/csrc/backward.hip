@@ -95,7 +95,8 @@ __global__ __launch_bounds__(kHomeThreads) void route_bwd_home_kernel(const int3
 }
 
 // alpha n f_i / T (Eq. 5, f fixed) + mu (ln(P_i / D_l[i]) + 1) / T (Eq. 6 through P), from the tokens per home node and the
-// experts per node
+// experts per node.  P_i = 0 (a masked expert): p_i is 0 for every token and 0 ln 0 = 0, so Eq. 6 has no gradient there; its ln
+// would make 0 x inf of every token's.
 __device__ __forceinline__ float coef_of(int i, bool has_home, const int32_t* s_home, const int32_t* s_pernode,
                                          const int32_t* e2n, const int32_t* cnt, const float* Psum, int T, int E, int N,
                                          float alpha, float mu) {
@@ -104,7 +105,7 @@ __device__ __forceinline__ float coef_of(int i, bool has_home, const int32_t* s_
     const int nu = e2n ? e2n[i] : i / (E / N);
     const double Dl = (double)s_home[nu] / ((double)T * (double)s_pernode[nu]);
     const double P = (double)Psum[i] / T;
-    c += (double)mu * (log(P / Dl) + 1.0) / T;
+    if (P != 0.0) c += (double)mu * (log(P / Dl) + 1.0) / T;
   }
   return (float)c;
 }

@@ -126,3 +126,53 @@ def test_block_without_experts(env):
         assert (s.b.eid == 0).all() and torch.isnan(s.b.w).all()
         assert (s.b.slot[:20] >= 0).all() and (s.b.slot[20:] == -1).all()
         assert torch.isnan(s.b.y[:20]).all() and torch.equal(s.b.y[20:], s.xd[20:])
+
+
+def test_gradients_beside_masked_experts(env):
+    """locmoe_route_bwd with experts masked by -inf and the locality loss on (0 ln 0 = 0): the formula, which central differences
+    of the objective bear out.  With D = max |dw| + max |coef|: p is (E + 12) f off (above), <p, dp> (2 E + 14) f D, and three
+    roundings follow: (4 E + 42) f D; and in coef 80 additions of fp32 behind P, mu / T of them each."""
+    torch, lm, _ = env
+    for T, E, N in ((37, 6, 3), (5000, 12, 4)):     # one launch and three
+        print(f"[route_bwd masked] T={T} E={E}", flush=True)
+        rng = np.random.default_rng(T)
+        g, dw = rng.normal(size=(T, E)).astype(np.float32), rng.normal(size=T).astype(np.float32)
+        eps = np.where(np.arange(E) % 3 == 1, -np.inf, 0.1 * rng.normal(size=E)).astype(np.float32)
+        home, alpha, mu = rng.integers(0, N, T).astype(np.int32), 0.3, 0.2
+        desc = lm.make_desc(T, 8 * E, E, N, 8, T, relu=False, alpha=alpha, mu=mu)
+        i32, f32 = dict(dtype=torch.int32, device="cuda"), dict(dtype=torch.float32, device="cuda")
+        eid, w, cnt, Psum, stats = torch.empty(T, **i32), torch.empty(T, **f32), torch.empty(E, **i32), torch.empty(E, **f32), torch.empty(8, **f32)
+        n = lm.locmoe_workspace_bytes(desc)
+        gd, epsd, homed, dwd = (torch.from_numpy(a).cuda() for a in (g, eps, home, dw))
+        lm.locmoe_route(desc, gd, epsd, homed, None, eid, w, cnt, Psum, stats, torch.empty(n, dtype=torch.uint8, device="cuda"), n)
+        coef, dg = torch.empty(E, **f32), torch.empty(T, E, **f32)
+        lm.locmoe_route_bwd(desc, gd, epsd, homed, None, eid, cnt, Psum, dwd, coef, dg)
+        assert torch.isfinite(stats).all() and torch.isfinite(coef).all() and (Psum[1::3] == 0).all()
+        e, live = eid.cpu().numpy(), np.isfinite(eps)
+        assert live[e].all()
+        f = np.bincount(e, minlength=E) / T
+        Dl = np.repeat(np.bincount(home, minlength=N), E // N) / (T * (E // N))
+
+        def probs(G):
+            z = np.exp(G - G.max(axis=1, keepdims=True))
+            return z / z.sum(axis=1, keepdims=True)
+
+        def objective(G):
+            p = probs(G)
+            P = p.mean(axis=0)
+            return (dw * p[np.arange(T), e]).sum() + alpha * E * f @ P + mu * np.sum(P[live] * np.log(P[live] / Dl[live]))
+
+        G = (g + eps).astype(np.float64)
+        p = probs(G)
+        c = alpha * E * f / T
+        c[live] += mu * (np.log(p.mean(axis=0)[live] / Dl[live]) + 1) / T
+        dp = c[None, :] + dw[:, None] * (np.arange(E)[None, :] == e[:, None])
+        ref = p * (dp - (p * dp).sum(axis=1, keepdims=True))
+        for m, i in ((0, 0), (T // 2, 2), (T - 1, E - 1)):
+            step = np.zeros_like(G)
+            step[m, i] = 1e-5
+            assert abs((objective(G + step) - objective(G - step)) / 2e-5 - ref[m, i]) <= 1e-7
+        got = dg.double().cpu().numpy()
+        assert (got[:, ~live] == 0).all()
+        D = np.abs(dw).max() + np.abs(c).max()
+        assert (np.abs(got - ref) <= (4 * E + 42) * F * D + 80 * F * mu / T).all()

@@ -119,7 +119,7 @@ __device__ __forceinline__ void few_route(const FewRoute& r, const void* x, cons
       if (eps) v += eps[e];
       if (relu) v = fmaxf(v, 0.f);
       const float f = v == best ? 1.0f : __builtin_amdgcn_exp2f(-kLog2e * fabsf(v - best));  // (both may be -inf: a masked expert)
-      const bool more = v > best || at == E;  // (ascending e: ties stay with the lower)
+      const bool more = v > best;  // (ascending e: ties stay with the lower; a NaN is never the largest, but stays in z)
       z = more ? fmaf(z, f, 1.0f) : z + f;
       best = more ? v : best;
       at = more ? e : at;
@@ -140,8 +140,9 @@ __device__ __forceinline__ void few_route(const FewRoute& r, const void* x, cons
       top = take ? ov : top;
       who = take ? oa : who;
     }
-    const float sum = lanes_sum(at < E && (l & (L - 1)) == 0 ? z * __builtin_amdgcn_exp2f(kLog2e * (best - top)) : 0.f, S);
-    if (l == 0 && m0 < T) { s_eid[m] = who; s_w[m] = 1.0f / sum; }
+    // (lanes without an expert have z = 0; nothing above -inf at all: expert 0 and NaN, as locmoe_route)
+    const float sum = lanes_sum((l & (L - 1)) == 0 ? z * __builtin_amdgcn_exp2f(kLog2e * (best - top)) : 0.f, S);
+    if (l == 0 && m0 < T) { s_eid[m] = who < E ? who : 0; s_w[m] = 1.0f / sum; }
   }
 }
 

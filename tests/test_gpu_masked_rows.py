@@ -176,3 +176,73 @@ def test_gradients_beside_masked_experts(env):
         assert (got[:, ~live] == 0).all()
         D = np.abs(dw).max() + np.abs(c).max()
         assert (np.abs(got - ref) <= (4 * E + 42) * F * D + 80 * F * mu / T).all()
+
+
+def few(env, T, d, E, C, relu, dtype="bf16"):
+    """locmoe_layer_few's call with weights of ones: f(x, g) -> eid, w, slot, y."""
+    torch, lm, _ = env
+    desc = lm.make_desc(T, d, E, 1, 8, C, dtype, relu)
+    W_in, W_out = (torch.ones(E, *s, dtype=torch.bfloat16, device="cuda") for s in ((8, d), (d, 8)))
+    n = lm.locmoe_layer_few_workspace_bytes(desc)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+
+    def call(x, g=None):
+        i32 = dict(dtype=torch.int32, device="cuda")
+        eid, slot, w, y = torch.full((T,), 99, **i32), torch.full((T,), 99, **i32), torch.full((T,), 7.0, device="cuda"), torch.full_like(x, 7.0)
+        lm.locmoe_layer_few(desc, x, g, None, W_in, W_out, True, eid, w, slot, y, ws, n)
+        return eid, w, slot, y
+    return desc, call
+
+
+@pytest.mark.parametrize("T,E", [(1, 1), (1, 4), (9, 5), (7, 12), (64, 16), (33, 96), (2, 257), (64, 1024)])
+@pytest.mark.parametrize("relu", [False, True])
+def test_few_tokens(env, T, E, relu):
+    """The layer for a few tokens takes the experts that locmoe_route takes, NaN or not."""
+    torch, lm, _ = env
+    print(f"[few masked] T={T} E={E} relu={relu}", flush=True)
+    rng = np.random.default_rng(T + E)
+    C = max(1, T // 2)
+    _, call = few(env, T, 8 * E, E, C, relu)
+    x = torch.ones(T, 8 * E, dtype=torch.bfloat16, device="cuda")
+    # NaN in each place of a row by itself too: the first of a lane's experts, a later one, the only one above the rest
+    sets = [rows(rng, T, E)]
+    for at in range(0, E, max(1, E // 5)):
+        g = rng.uniform(-4.0, 4.0, (T, E)).astype(np.float32)
+        g[::2, at] = np.nan
+        sets.append(g)
+    for g in sets:
+        eid, w, slot, y = call(x, torch.from_numpy(g).cuda())
+        want, score = expected(g, relu)
+        assert np.array_equal(eid.cpu().numpy(), want)
+        place = [m if (want[:m] == want[m]).sum() < C else -1 for m in range(T)]
+        assert slot.tolist() == place
+        got = w.double().cpu().numpy()
+        assert np.array_equal(np.isnan(got), np.isnan(score))
+        live = ~np.isnan(score)
+        assert (np.abs(got - score)[live] <= (E + 12) * F * score[live]).all()
+        dead = torch.tensor([p >= 0 and not l for p, l in zip(place, live)], device="cuda")
+        assert torch.isnan(y[dead]).all() and torch.isfinite(y[~dead]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("relu", [False, True])
+def test_nan_in_x_of_a_few_tokens(env, relu, dtype):
+    """Gating values formed by the layer: a NaN in x reaches its own block's value, so the token goes where locmoe_gate and
+    locmoe_route send it, and no other token changes."""
+    torch, lm, _ = env
+    for T, d, E in ((1, 64, 8), (5, 96, 12), (17, 600, 50), (64, 1024, 64)):
+        print(f"[few NaN in x] T={T} d={d} E={E} relu={relu} {dtype}", flush=True)
+        gen = torch.Generator(device="cuda").manual_seed(T)
+        desc, call = few(env, T, d, E, T, relu, dtype)
+        x = torch.randn(T, d, generator=gen, device="cuda").to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+        clean = call(x)
+        for m, at in ((0, 0), (T // 2, d // 2), (T - 1, d - 1)):
+            bad = x.clone()
+            bad[m, at] = float("nan")
+            eid, w, slot, y = call(bad)
+            g, rest = torch.empty(T, E, device="cuda"), [k for k in range(T) if k != m]
+            lm.locmoe_gate(desc, bad, g)
+            want, _ = expected(g.cpu().numpy(), relu)
+            assert eid.tolist() == want.tolist() and slot.tolist() == list(range(T))
+            assert bool(torch.isnan(w[m])) == (not relu) and torch.isnan(y[m]).all()
+            assert torch.equal(w[rest], clean[1][rest]) and torch.isfinite(y[rest]).all()

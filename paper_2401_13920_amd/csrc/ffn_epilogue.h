@@ -69,6 +69,9 @@ __device__ __forceinline__ float gelu_grad_bf16(float v) {
 
 // The larger value, or NaN if either is one
 __device__ __forceinline__ float maximum(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+// GeLU(v) = v Phi(v) for outputs that are rounded to bf16, beside a GeLU'(v) that uses the same Phi.  Below -6 the polynomial's
+// Phi stays at Phi(-6), and so must v: the product is above -6e-9, as gelu_bf16's.
+__device__ __forceinline__ float gelu_by_cdf_bf16(float v) { return maximum(v, -kGeluXMax) * normal_cdf_bf16(v); }
 // Four values of a lane, each to be the largest of four lanes 16 apart.  The four are reduced together: the lanes of 16-lane
 // row r end with the result of value quad_of_row(r), in 3 exchanges instead of 8; spread_rows takes such a register apart again.
 __device__ __forceinline__ constexpr int quad_of_row(int r) { return (r >> 1) | ((r & 1) << 1); }
@@ -149,8 +152,8 @@ struct Row8 {
       const float z0 = (float)(int8_t)q[i] * s, z1 = (float)(int8_t)(q[i] >> 8) * s;
       const float z2 = (float)(int8_t)(q[i] >> 16) * s, z3 = (float)(int8_t)(q[i] >> 24) * s;
       const f32x4 a = acc(i);
-      *(uint2*)(Hr + i * STEP) = make_uint2(pack_bf16x2(z0 * normal_cdf_bf16(z0), z1 * normal_cdf_bf16(z1)),
-                                            pack_bf16x2(z2 * normal_cdf_bf16(z2), z3 * normal_cdf_bf16(z3)));
+      *(uint2*)(Hr + i * STEP) = make_uint2(pack_bf16x2(gelu_by_cdf_bf16(z0), gelu_by_cdf_bf16(z1)),
+                                            pack_bf16x2(gelu_by_cdf_bf16(z2), gelu_by_cdf_bf16(z3)));
       *(uint2*)(Cr + i * STEP) = make_uint2(pack_bf16x2(a[0] * gelu_grad_bf16(z0), a[1] * gelu_grad_bf16(z1)),
                                             pack_bf16x2(a[2] * gelu_grad_bf16(z2), a[3] * gelu_grad_bf16(z3)));
     }

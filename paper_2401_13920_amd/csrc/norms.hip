@@ -105,7 +105,7 @@ __global__ __launch_bounds__(threads_of<LPR>()) void norm_gate_kernel(const uint
   __shared__ float sm[THREADS / kWave];
   extern __shared__ float part[];  // kChunks: [RPB][chunks], kElements: [RPB][chunks V]
   const int rg = threadIdx.x / LPR, l = threadIdx.x % LPR;
-  const unsigned m = blockIdx.x * RPB + rg;  // (T fills 31 bits: the last work-group's rows may not fit them)
+  const unsigned m = blockIdx.x * RPB + rg;
   const bool live = m < (unsigned)T;
   const uint4* src = x + (size_t)(live ? m : T - 1) * chunks;
   uint4 v[CPL];
@@ -476,7 +476,20 @@ int norm_row(const locmoe_desc* p, NormRow* r) {
 }
 inline bool finite(float v) { return v - v == 0.0f; }
 
-inline int part_rows(int T, int rows_per_group) { return std::min(ceil_div(T, rows_per_group), kNormMaxParts); }
+// (T fills 31 bits: no sum with it that may not fit them)
+inline int part_rows(int T, int rows_per_group) { return std::min((T - 1) / rows_per_group + 1, kNormMaxParts); }
+
+// The forward kernels have a work-group for every few rows, and a launch takes fewer than 2^32 threads: f(first row, rows) for runs of
+// rows of 2^31 threads each.  (2^27 rows of up to 32 chunks, 2^21 of the longest)
+template <class S, class F>
+int by_runs(int T, F&& f) {
+  constexpr long long kRun = (1ll << 31) / S::kThreads * S::kRows;
+  for (long long m0 = 0; m0 < T; m0 += kRun) {
+    const int st = f((size_t)m0, (int)std::min<long long>(kRun, T - m0));
+    if (st != LOCMOE_OK) return st;
+  }
+  return LOCMOE_OK;
+}
 
 template <bool BF>
 int norm_gate_impl(const NormRow& row, const locmoe_desc* desc, const void* x, const float* gamma, float eps, void* xn,
@@ -492,9 +505,12 @@ int norm_gate_impl(const NormRow& row, const locmoe_desc* desc, const void* x, c
     static std::atomic<uint64_t> allowed[3];
     // (the limit without asking is 64 KiB, some of which are the kernel's own words)
     if (lds > 60000 && !allow_lds((const void*)kern, kMaxNormLds, allowed[form])) return (int)LOCMOE_ERR_HIP;
-    hipLaunchKernelGGL(kern, dim3(ceil_div(T, S::kRows)), dim3(S::kThreads), lds, s, (const uint4*)x, gamma, (uint4*)xn, rstd,
-                       g, T, row.chunks, E, row.blk, row.inv_d, eps);
-    return launch_status();
+    return by_runs<S>(T, [&](size_t m0, int n) {
+      hipLaunchKernelGGL(kern, dim3(ceil_div(n, S::kRows)), dim3(S::kThreads), lds, s, (const uint4*)x + m0 * row.chunks, gamma,
+                         (uint4*)xn + m0 * row.chunks, rstd ? rstd + m0 : nullptr, g ? g + m0 * E : nullptr, n, row.chunks, E,
+                         row.blk, row.inv_d, eps);
+      return launch_status();
+    });
   });
 }
 
@@ -504,9 +520,12 @@ int combine_norm_impl(const NormRow& row, int T, const void* out, const int32_t*
   return with_forward_row(row.chunks, [&](auto shape) {
     using S = decltype(shape);
     auto kern = post ? combine_norm_kernel<BF, S::LPR, S::CPL, true> : combine_norm_kernel<BF, S::LPR, S::CPL, false>;
-    hipLaunchKernelGGL(kern, dim3(ceil_div(T, S::kRows)), dim3(S::kThreads), 0, s, (const uint4*)out, slot, w,
-                       (const uint4*)res, gamma, (uint4*)y, rstd, T, row.chunks, row.inv_d, eps, scale);
-    return launch_status();
+    return by_runs<S>(T, [&](size_t m0, int n) {
+      hipLaunchKernelGGL(kern, dim3(ceil_div(n, S::kRows)), dim3(S::kThreads), 0, s, (const uint4*)out, slot + m0, w + m0,
+                         (const uint4*)res + m0 * row.chunks, gamma, (uint4*)y + m0 * row.chunks, rstd ? rstd + m0 : nullptr, n,
+                         row.chunks, row.inv_d, eps, scale);
+      return launch_status();
+    });
   });
 }
 

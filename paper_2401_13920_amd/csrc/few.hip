@@ -7,9 +7,12 @@
 // Bound by the stream of weights: 4 d h bytes per expert with tokens.  Weight rows feed the MFMA's A operand, 16 rows x 32 k a
 // KiB straight from memory into registers; a group's tokens are the columns, 16 per MFMA, fetched from L2.  A tile of 16
 // weight rows is shared by up to eight waves of a work-group, each with its part of K, where there are fewer tiles than waves;
-// their sums meet in LDS and are added in order.  Measured (both kernels, as in a decoder's loop): 64 tokens on 20 of 64 experts,
-// d = 4096, h = 16384, 5.4 GB of weights: 890 us packed, 915 row-major, 6.0 TB/s (a copy-free read of as much: 6.3 to 7.0); one token,
-// d = 1024, h = 4096, 16.8 MB: 11.6 us, of which the launches, the routing and a round trip to memory each are most.
+// their sums meet in LDS and are added in order.  Measured (both kernels, one call after another): 64 tokens on 16 to 27 of 64
+// experts in turn, gating values given, d = 4096, h = 16384, 4.3 to 7.2 GB of weights: 6.5 to 6.6 TB/s packed, 5.7 to 6.5 row-major (a
+// copy-free read of as much: 6.3 to 7.0); one token, d = 1024, h = 4096, 16.8 MB: 11.5 us, of which the launches, the routing
+// and a round trip to memory each are most.  Far from the stream's rate: many tokens on one expert, and fp32 storage, where the
+// tokens' operands, which every tile fetches again from L2, are several times the weights (64 tokens on one expert,
+// d = 2048, h = 8192, 67 MB: 67 us).
 //
 // bf16 storage: H is rounded to bf16, as in the layer's other path.  fp32 storage: the activations and H keep all 24 bits: a
 // value is the sum of three bf16 parts, whose exact products with the bf16 weights are summed in fp32.
@@ -294,7 +297,8 @@ __device__ __forceinline__ void few_dot(f32x4 (&acc)[NB], const char* __restrict
   };
   // Whole turns in a cycle that begins at a place of its own in neighbouring blocks of packed rows (tiles of row-major lines): in
   // step, all waves read at multiples of a power of two, which are few of the memory's channels (packed, d = 4096, h = 16384, 20
-  // experts: 952 -> 890 us).
+  // experts: 952 -> 890 us).  With fewer turns than places all start together: there, with 17, 18, 21, 22, 25 or 26 experts, where
+  // two or eight waves share a tile and have eight turns each (6.5 to 6.6 TB/s, as the others).
   const int full = LINES ? s1 : min(s1, k_seg / 32), turns = max(full - s0, 0) / D;
   int at = s0 + (PACKED ? ((tile >> 4) & 15) * (turns >> 4) : LINES ? (tile & 7) * (turns >> 3) : 0) * D;
   for (int i = 0; i < turns; ++i) {

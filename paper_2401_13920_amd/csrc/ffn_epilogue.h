@@ -19,8 +19,10 @@ constexpr bool kept8(int epi) { return epi == kEpiGeluSave8 || epi == kEpiGeluGr
 // block lies in four lanes of one wave whatever the tile.  At 9 bits a value it is 0.3 to 0.5 % off (root mean square, of
 // normally distributed z), where 8 bits with an exponent each (e4m3) are 2.6 % off.
 // A block with an infinity or a NaN reads back as NaN; one below 127 x 2^-126 as zeros.
-// Time, T = 32 768, d = 2048, h = 8192, E = 32, 17 563 rows: the first GEMM 632 us (with Z kept in bf16 662: it stores 0.72 GB for
-// 1.15), the two GEMMs of the data gradients 1 260 (1 204: H is formed and stored again, 0.29 GB).  Bound by the GEMM.
+// Time, T = 32 768, d = 2048, h = 8192, E = 32, 17 598 rows: the first GEMM 627 us (with Z kept in bf16 637: it stores 0.72 GB for
+// 1.15; with nothing kept 560), the two GEMMs of the data gradients 1 255 (1 215: H is formed and stored again, 0.29 GB);
+// T = 8192, d = 1024, h = 4096, E = 16: 121 (123; 79 to 98) and 235 (228).  A store instruction writes pieces of 16 and 32 bytes of
+// 16 rows, which the GEMM's loop does not cover where a work-group has a compute unit to itself.
 struct Act8 {
   int8_t* q;       // [rows][N]
   uint16_t* unit;  // [rows][ceil(N / 16)] bf16

@@ -4,7 +4,10 @@
 //   locmoe_combine_norm_bwd   its gradients: dout, dw, dgamma
 //   locmoe_dispatch_norm_bwd  dxn = dsend[slot] + (E/d) dg, and the norm's backward: dx, dgamma
 // Every row is read once, held in registers between the sum over it and its use, and written once.  LPR lanes share a row,
-// CPL 16-byte chunks each.  All of it is bound by memory, loaded and stored past the caches: with T = 65 536 tokens, d = 4096, E = 64,
+// CPL 16-byte chunks each.  (Backward, rows of more than 32 KiB: gamma and its gradient do not fit beside the row in the 128
+// registers of a work-group of 1 024, and spill: bf16, d = 32 768, 4 096 tokens 511 and 745 us, 1.6 and 1.4 TB/s, where d = 16 384
+// with 8 192 tokens takes 181 and 208.  fp32 rows, and bf16 ones of 16 to 32 KiB whose blocks are no whole chunks, spill a few
+// words: 5.1 and 5.5 TB/s, 4.2 and 4.9.)  All of it is bound by memory, loaded and stored past the caches: with T = 65 536 tokens, d = 4096, E = 64,
 // bf16, 31 200 of them kept, norm_gate takes 196 us (1.09 GB, 5.6 TB/s), combine_norm 217 (1.34 GB, 6.2), combine_norm_bwd 158
 // (0.79 GB, 5.0) and dispatch_norm_bwd 323 (1.90 GB, 5.9); a plain copy reaches 5.7.  With 64 tokens of d = 1024 each takes 3.4 us,
 // less than its launch from the host.
